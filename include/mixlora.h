@@ -332,6 +332,108 @@ MIXLORA_API int mixlora_lora_linear_backward(const mixlora_linear_dims *dims, co
                                              size_t workspace_bytes, void *dx, float *dA,
                                              float *dB, void *stream);
 
+/* ---- 4-bit frozen matrices --------------------------------------------------------------------
+ * W' [d_out, d_in] = scale x level, with 4-bit floating-point codes (bit 3 the sign, levels 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6) and one bf16 scale per group of 32, 64 or 128 consecutive inputs of a row (the last
+ * group of a row may be short).  Layout of the two arrays, for programs that fill them from a checkpoint:
+ * a tile is 16 rows x 128 inputs, the tiles of a block of 16 rows follow one another, row blocks too.
+ *   codes : 1024 bytes per tile; of row i (of the 16), input 32 b + 8 h + e (b, h < 4, e < 8) is at byte
+ *           16 (16 h + i) + 4 b + e / 2, in the low half of the byte for even e.
+ *   scales: per tile [16 rows][128 / group].
+ * Codes and scales past the last row or input have to be zero.  mixlora_q4_quantize fills both: the scale is
+ * the smallest number of six significant bits that is at least a sixth of the group's largest magnitude
+ * (0 where that is below 2^-100; NaN, and so every value of the group, where it is 2^127 or more or not a
+ * number), the code the nearest level, ties to the even code.  With such scales W' is exact in bf16 and every
+ * path below computes with the same W'; scales of more significant bits are allowed, the bf16 products then
+ * may see scale x level rounded to bf16.
+ * Limits: d_out % 8 == 0, d_in % 8 == 0, fewer than 2^31 tiles.  dtype: of W.                    */
+typedef struct {
+  void *codes;   /* device, mixlora_q4_code_bytes(d_out, d_in) bytes, 16-byte aligned           */
+  void *scales;  /* device bf16, mixlora_q4_scale_bytes(d_out, d_in, group) bytes, 16-byte aligned */
+  int32_t group;
+} mixlora_q4;
+
+/* Bytes of the two arrays (0 for invalid sizes).  Host-only. */
+MIXLORA_API size_t mixlora_q4_code_bytes(int32_t d_out, int32_t d_in);
+MIXLORA_API size_t mixlora_q4_scale_bytes(int32_t d_out, int32_t d_in, int32_t group);
+MIXLORA_API int mixlora_q4_quantize(const void *W, int32_t dtype, int32_t d_out, int32_t d_in,
+                                    const mixlora_q4 *q4, void *stream);
+/* W [d_out, d_in], or with transposed = 1 [d_in, d_out]: what mixlora_ffn_forward / _backward and the other
+ * entry points take as a frozen matrix or as its transposed copy (one buffer can serve all layers). */
+MIXLORA_API int mixlora_q4_dequantize(const mixlora_q4 *q4, int32_t d_out, int32_t d_in,
+                                      int32_t transposed, void *W, int32_t dtype, void *stream);
+
+/* ---- Dropout on an adapter's input, without a stored mask --------------------------------------
+ * D(x)[t, c] = 0 where the 16 bits of (t, c) are below P, else x[t, c] * 65536 / (65536 - P), with
+ * P = floor(65536 p + 1/2).  The bits come from Philox4x32 (Salmon et al. 2011) with seven rounds: counter
+ * words {c / 8, t, offset low, offset high}, key {seed low, seed high}; column c takes half (c % 2) (0 = low)
+ * of word c % 8 / 2 of the result.  One (seed, offset) pair per layer and step; the backward call has to get
+ * the forward call's.  step: device pointer or NULL; its value is added to offset when the kernels run, so
+ * that a captured graph draws a new mask on every replay if the program advances it in between.
+ * Errors: MIXLORA_E_SHAPE for p outside [0, 1) or p so close to 1 that P is 65536, MIXLORA_E_ALIGN for a
+ * step that is not 8-byte aligned.  A NULL struct or P = 0 means no dropout.                       */
+typedef struct {
+  float p;
+  uint64_t seed, offset;
+  const uint64_t *step;
+} mixlora_dropout;
+
+/* ---- LoRA linear on a 4-bit matrix, and with dropout --------------------------------------------
+ *   y = x W^T + s (D(x) A^T) B^T ;  dx = dy W + D'(s (dy B) A),  dA = s (dy B)^T D(x),
+ *   dB = s dy^T (D(x) A^T), where D' drops and scales the elements that D does.
+ * Shapes, limits, workspace rules and errors as in mixlora_lora_linear_forward / _backward (group has to be
+ * 32, 64 or 128: MIXLORA_E_SHAPE).  The rank-r factors keep their 24 bits in the sums of dA and dB.
+ * The mixlora_lora_dropout calls take an ordinary frozen matrix (W_T optional as there). */
+MIXLORA_API size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_t group,
+                                                     int for_backward);
+MIXLORA_API int mixlora_q4_linear_forward(const mixlora_linear_dims *dims, const mixlora_q4 *q4,
+                                          const void *A, const void *B, const mixlora_dropout *dropout,
+                                          const void *x, void *y, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+MIXLORA_API int mixlora_q4_linear_backward(const mixlora_linear_dims *dims, const mixlora_q4 *q4,
+                                           const void *A, const void *B, const mixlora_dropout *dropout,
+                                           const void *x, const void *dy, void *workspace,
+                                           size_t workspace_bytes, void *dx, float *dA, float *dB,
+                                           void *stream);
+MIXLORA_API size_t mixlora_lora_dropout_workspace_bytes(const mixlora_linear_dims *dims, int for_backward);
+MIXLORA_API int mixlora_lora_dropout_forward(const mixlora_linear_dims *dims, const void *W, const void *A,
+                                             const void *B, const mixlora_dropout *dropout, const void *x,
+                                             void *y, void *workspace, size_t workspace_bytes, void *stream);
+MIXLORA_API int mixlora_lora_dropout_backward(const mixlora_linear_dims *dims, const void *W,
+                                              const void *W_T, const void *A, const void *B,
+                                              const mixlora_dropout *dropout, const void *x, const void *dy,
+                                              void *workspace, size_t workspace_bytes, void *dx, float *dA,
+                                              float *dB, void *stream);
+
+/* ---- Router over padded batches: routing, Eq. 8-9, z-loss, and the gradient of the logits --------
+ * For logits z [T, N] (dims.dtype) and a mask of T bytes (0 = padding; NULL = every token counts):
+ *   p = softmax(z); the k largest logits are kept (equal ones: the lower index; NaN ranks with -inf);
+ *   topk_w = their p over its sum; n = tokens that count;
+ *   balance = balance_coeff * N * sum_i F_i P_i  with F, P of Eq. 9 over those tokens (aux_mode as above);
+ *   z = z_coeff / n * sum_t (log sum_i exp z_ti)^2.
+ * out: loss [3] float32 = {balance + z, balance, z}; counts [N] int32 = pairs per expert; topk_idx [T, k]
+ *      int32 and topk_w [T, k] float32.  A token that does not count has indices -1 and weights 0, and its
+ *      logits, NaN included, reach nothing.  No token: losses and counts are 0.
+ * Limits: 1 <= k <= N <= 64, T * k < 2^24; logits are 16-byte aligned, token_mask need not be. */
+typedef struct {
+  int32_t T, N, k;
+  float balance_coeff, z_coeff;
+  int32_t aux_mode, dtype;
+} mixlora_router_dims;
+MIXLORA_API size_t mixlora_router_loss_workspace_bytes(const mixlora_router_dims *dims);
+MIXLORA_API int mixlora_router_loss_forward(const mixlora_router_dims *dims, const void *logits,
+                                            const unsigned char *token_mask, float *loss, int32_t *counts,
+                                            int32_t *topk_idx, float *topk_w, void *workspace,
+                                            size_t workspace_bytes, void *stream);
+/* dlogits [T, N] (dims.dtype) of  d_balance * balance + d_z * z + <topk_w, d_topk_w>  on the workspace that the
+ * forward call filled.  d_topk_w [T, k] float32 may be NULL; topk_idx (the forward's) goes with it.  F carries
+ * no gradient.  Zeros for a token that does not count. */
+MIXLORA_API int mixlora_router_loss_backward(const mixlora_router_dims *dims, const void *logits,
+                                             const unsigned char *token_mask, const int32_t *topk_idx,
+                                             const float *d_topk_w, float d_balance, float d_z,
+                                             void *workspace, size_t workspace_bytes, void *dlogits,
+                                             void *stream);
+
 /* ---- AdamW step on adapter parameters (the optimiser named in the paper's hyper-parameter
  * table; decoupled weight decay):
  *   p <- p (1 - lr wd);  m <- b1 m + (1-b1) g;  v <- b2 v + (1-b2) g^2;

@@ -30,7 +30,13 @@ EXPORTS = ("mixlora_workspace_bytes", "mixlora_ffn_forward", "mixlora_ffn_backwa
            "mixlora_lora_linear_forward", "mixlora_lora_linear_backward", "mixlora_adamw_step",
            "mixlora_schedule_workspace_bytes", "mixlora_ffn_forward_schedule",
            "mixlora_ffn_backward_schedule", "mixlora_dora_workspace_bytes",
-           "mixlora_dora_forward", "mixlora_dora_backward", "mixlora_ffn_forward_static")
+           "mixlora_dora_forward", "mixlora_dora_backward", "mixlora_ffn_forward_static",
+           "mixlora_q4_code_bytes", "mixlora_q4_scale_bytes", "mixlora_q4_quantize",
+           "mixlora_q4_dequantize", "mixlora_q4_linear_workspace_bytes",
+           "mixlora_q4_linear_forward", "mixlora_q4_linear_backward",
+           "mixlora_lora_dropout_workspace_bytes", "mixlora_lora_dropout_forward",
+           "mixlora_lora_dropout_backward", "mixlora_router_loss_workspace_bytes",
+           "mixlora_router_loss_forward", "mixlora_router_loss_backward")
 
 
 class Dims(C.Structure):
@@ -55,6 +61,19 @@ class Grads(C.Structure):
 class LinearDims(C.Structure):
     _fields_ = [("T", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("r", C.c_int32),
                 ("lora_scale", C.c_float), ("dtype", C.c_int32)]
+
+
+class Q4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("group", C.c_int32)]
+
+
+class Dropout(C.Structure):
+    _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64), ("step", C.c_void_p)]
+
+
+class RouterDims(C.Structure):
+    _fields_ = [("T", C.c_int32), ("N", C.c_int32), ("k", C.c_int32), ("balance_coeff", C.c_float),
+                ("z_coeff", C.c_float), ("aux_mode", C.c_int32), ("dtype", C.c_int32)]
 
 
 class AdamW(C.Structure):
@@ -160,6 +179,24 @@ def load():
     lib.mixlora_lora_linear_backward.restype = C.c_int
     lib.mixlora_lora_linear_backward.argtypes = [C.POINTER(LinearDims), vp, vp, vp, vp, vp, vp, vp,
                                                  sz, vp, vp, vp, vp]
+    for name in ("mixlora_q4_code_bytes", "mixlora_q4_scale_bytes", "mixlora_q4_linear_workspace_bytes",
+                 "mixlora_lora_dropout_workspace_bytes", "mixlora_router_loss_workspace_bytes"):
+        getattr(lib, name).restype = sz
+    lib.mixlora_q4_code_bytes.argtypes = [i32, i32]
+    lib.mixlora_q4_scale_bytes.argtypes = [i32, i32, i32]
+    lib.mixlora_q4_quantize.argtypes = [vp, i32, i32, i32, C.POINTER(Q4), vp]
+    lib.mixlora_q4_dequantize.argtypes = [C.POINTER(Q4), i32, i32, i32, vp, i32, vp]
+    lin, q4, drop = C.POINTER(LinearDims), C.POINTER(Q4), C.POINTER(Dropout)
+    lib.mixlora_q4_linear_workspace_bytes.argtypes = [lin, i32, C.c_int]
+    lib.mixlora_q4_linear_forward.argtypes = [lin, q4, vp, vp, drop, vp, vp, vp, sz, vp]
+    lib.mixlora_q4_linear_backward.argtypes = [lin, q4, vp, vp, drop, vp, vp, vp, sz, vp, vp, vp, vp]
+    lib.mixlora_lora_dropout_workspace_bytes.argtypes = [lin, C.c_int]
+    lib.mixlora_lora_dropout_forward.argtypes = [lin, vp, vp, vp, drop, vp, vp, vp, sz, vp]
+    lib.mixlora_lora_dropout_backward.argtypes = [lin, vp, vp, vp, vp, drop, vp, vp, vp, sz, vp, vp, vp, vp]
+    rd = C.POINTER(RouterDims)
+    lib.mixlora_router_loss_workspace_bytes.argtypes = [rd]
+    lib.mixlora_router_loss_forward.argtypes = [rd, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mixlora_router_loss_backward.argtypes = [rd, vp, vp, vp, vp, f32, f32, vp, sz, vp, vp]
     lib.mixlora_adamw_step.restype = C.c_int
     lib.mixlora_adamw_step.argtypes = [C.POINTER(AdamW), C.c_int64, vp, vp, vp, vp, vp, i32, vp]
     lib.mixlora_mfma_probe.restype = C.c_int
@@ -389,6 +426,108 @@ def mixlora_lora_linear_backward(dims: LinearDims, W, W_T, A, B_, x, dy, workspa
                                              _ptr(dx), _ptr(dA), _ptr(dB), _stream(stream))
     if rc != 0:
         raise MixLoraError("mixlora_lora_linear_backward", rc)
+
+
+def make_q4(codes, scales, group: int) -> Q4:
+    """codes, scales: device tensors (or raw pointers) of mixlora_q4_code_bytes / _scale_bytes bytes."""
+    q = Q4(_ptr(codes), _ptr(scales), group)
+    q._keep = (codes, scales)
+    return q
+
+
+def make_dropout(p: float, seed: int, offset: int, step=None) -> Dropout:
+    """step: device tensor of one 64-bit integer that is added to offset when the kernels run, or None."""
+    d = Dropout(p, seed & (2 ** 64 - 1), offset & (2 ** 64 - 1), _ptr(step))
+    d._keep = step
+    return d
+
+
+def _opt(struct):
+    return None if struct is None else C.byref(struct)
+
+
+def mixlora_q4_code_bytes(d_out: int, d_in: int) -> int:
+    return int(load().mixlora_q4_code_bytes(d_out, d_in))
+
+
+def mixlora_q4_scale_bytes(d_out: int, d_in: int, group: int) -> int:
+    return int(load().mixlora_q4_scale_bytes(d_out, d_in, group))
+
+
+def mixlora_q4_quantize(W, dtype: int, d_out: int, d_in: int, q4: Q4, stream=None) -> None:
+    rc = load().mixlora_q4_quantize(_ptr(W), dtype, d_out, d_in, _opt(q4), _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_q4_quantize", rc)
+
+
+def mixlora_q4_dequantize(q4: Q4, d_out: int, d_in: int, transposed: bool, W, dtype: int, stream=None) -> None:
+    rc = load().mixlora_q4_dequantize(_opt(q4), d_out, d_in, int(transposed), _ptr(W), dtype, _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_q4_dequantize", rc)
+
+
+def mixlora_q4_linear_workspace_bytes(dims: LinearDims, group: int, for_backward: bool) -> int:
+    return int(load().mixlora_q4_linear_workspace_bytes(C.byref(dims), group, int(bool(for_backward))))
+
+
+def mixlora_q4_linear_forward(dims: LinearDims, q4: Q4, A, B_, dropout: Optional[Dropout], x, y, workspace,
+                              workspace_bytes: int, stream=None) -> None:
+    rc = load().mixlora_q4_linear_forward(C.byref(dims), _opt(q4), _ptr(A), _ptr(B_), _opt(dropout), _ptr(x),
+                                          _ptr(y), _ptr(workspace), workspace_bytes, _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_q4_linear_forward", rc)
+
+
+def mixlora_q4_linear_backward(dims: LinearDims, q4: Q4, A, B_, dropout: Optional[Dropout], x, dy, workspace,
+                               workspace_bytes: int, dx, dA, dB, stream=None) -> None:
+    rc = load().mixlora_q4_linear_backward(C.byref(dims), _opt(q4), _ptr(A), _ptr(B_), _opt(dropout), _ptr(x),
+                                           _ptr(dy), _ptr(workspace), workspace_bytes, _ptr(dx), _ptr(dA),
+                                           _ptr(dB), _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_q4_linear_backward", rc)
+
+
+def mixlora_lora_dropout_workspace_bytes(dims: LinearDims, for_backward: bool) -> int:
+    return int(load().mixlora_lora_dropout_workspace_bytes(C.byref(dims), int(bool(for_backward))))
+
+
+def mixlora_lora_dropout_forward(dims: LinearDims, W, A, B_, dropout: Optional[Dropout], x, y, workspace,
+                                 workspace_bytes: int, stream=None) -> None:
+    rc = load().mixlora_lora_dropout_forward(C.byref(dims), _ptr(W), _ptr(A), _ptr(B_), _opt(dropout), _ptr(x),
+                                             _ptr(y), _ptr(workspace), workspace_bytes, _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_lora_dropout_forward", rc)
+
+
+def mixlora_lora_dropout_backward(dims: LinearDims, W, W_T, A, B_, dropout: Optional[Dropout], x, dy, workspace,
+                                  workspace_bytes: int, dx, dA, dB, stream=None) -> None:
+    rc = load().mixlora_lora_dropout_backward(C.byref(dims), _ptr(W), _ptr(W_T), _ptr(A), _ptr(B_), _opt(dropout),
+                                              _ptr(x), _ptr(dy), _ptr(workspace), workspace_bytes, _ptr(dx),
+                                              _ptr(dA), _ptr(dB), _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_lora_dropout_backward", rc)
+
+
+def mixlora_router_loss_workspace_bytes(dims: RouterDims) -> int:
+    return int(load().mixlora_router_loss_workspace_bytes(C.byref(dims)))
+
+
+def mixlora_router_loss_forward(dims: RouterDims, logits, token_mask, loss, counts, topk_idx, topk_w, workspace,
+                                workspace_bytes: int, stream=None) -> None:
+    rc = load().mixlora_router_loss_forward(C.byref(dims), _ptr(logits), _ptr(token_mask), _ptr(loss),
+                                            _ptr(counts), _ptr(topk_idx), _ptr(topk_w), _ptr(workspace),
+                                            workspace_bytes, _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_router_loss_forward", rc)
+
+
+def mixlora_router_loss_backward(dims: RouterDims, logits, token_mask, topk_idx, d_topk_w, d_balance: float,
+                                 d_z: float, workspace, workspace_bytes: int, dlogits, stream=None) -> None:
+    rc = load().mixlora_router_loss_backward(C.byref(dims), _ptr(logits), _ptr(token_mask), _ptr(topk_idx),
+                                             _ptr(d_topk_w), float(d_balance), float(d_z), _ptr(workspace),
+                                             workspace_bytes, _ptr(dlogits), _stream(stream))
+    if rc != 0:
+        raise MixLoraError("mixlora_router_loss_backward", rc)
 
 
 def mixlora_adamw_step(h: AdamW, n: int, param, grad, m, v, lowp=None, lowp_dtype: int = BF16,

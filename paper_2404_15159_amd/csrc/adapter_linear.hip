@@ -1,0 +1,424 @@
+// LoRA linear with dropout on the adapter's input, on an ordinary or on a 4-bit frozen matrix:
+//   y = x W^T + s (D(x) A^T) B^T,   dx = dy W + D'(s (dy B) A),   dA = s (dy B)^T D(x),   dB = s dy^T (D(x) A^T)
+// D drops elements and scales the others (dropout.h makes the mask from counters wherever it is needed),
+// D' drops the same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen
+// product as an extra K segment, in three bf16 pieces that hold all of its 24 bits, in the backward too
+// where there is no dropout; with dropout the product is made in fp32 and the masked term is added where it
+// is rounded, so that a result is rounded once.  The gradient sums take the rank-r factor in three pieces as
+// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h).
+#include "common.h"
+#include "q4.h"
+#include "rank_project.h"
+
+#include <cmath>
+#include <initializer_list>
+
+using namespace mixlora;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+inline size_t up(size_t v) { return (v + ALIGN - 1) / ALIGN * ALIGN; }
+inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+struct Layout {
+  int rp, ldT;                            // rank rounded up to a multiple of 8; pitch of the transposed factors
+  size_t padA, padB, P, P_T, offs;        // kept for the backward
+  size_t ext, ext_B, gemm_part, xd;       // scratch of either direction
+  size_t W, fwd_end;
+  size_t W_T, Bt, At, V, V_T, dx32, partials, padgA, padgB, bwd_end;
+  size_t gemm_floats, partial_floats;
+};
+
+// q4: room for the widened matrix.  The scratch of the two directions overlaps.
+Layout make_layout(const mixlora_linear_dims &D, bool q4) {
+  Layout L{};
+  const size_t T = D.T, di = D.d_in, dn = D.d_out, r = (D.r + 7) & ~7;
+  const bool bf16 = D.dtype == MIXLORA_BF16, padded = (int)r != D.r;
+  const size_t E = bf16 ? 2 : 4, wide = di > dn ? di : dn;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = up(o + bytes); return at; };
+  L.rp = (int)r;
+  L.ldT = (int)((T + 15) / 16 * 16 + 16);
+  L.padA = take(padded ? r * di * E : 0);
+  L.padB = take(padded ? dn * r * E : 0);
+  L.P = take(T * r * 4);
+  L.P_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
+  L.offs = take(2 * 4);
+  L.ext = take(bf16 ? T * 3 * r * 2 : 0);
+  L.ext_B = take(bf16 ? wide * 3 * r * 2 : 0);
+  {   // partial tiles of products cut along K: at most one tile per CU
+    const size_t slices = wide / 64 / 4, tiles = (T / 192 + 1) * (wide / 256 + 1) * slices;
+    L.gemm_floats = bf16 && slices >= 2 ? GEMM_SCRATCH_FLOATS / 256 * (tiles < 256 ? tiles : 256) : 0;
+    L.gemm_part = take(L.gemm_floats * 4);
+  }
+  L.xd = take(bf16 ? 0 : T * di * E);
+  const size_t scratch = o;
+  L.W = take(q4 ? di * dn * E : 0);
+  L.fwd_end = o;
+  o = scratch;
+  L.W_T = take(di * dn * E);
+  L.Bt = take(r * dn * E);
+  L.At = take(di * r * E);
+  L.V = take(T * r * 4);
+  L.V_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
+  L.dx32 = take(bf16 ? T * di * 4 : 0);
+  L.partial_floats = bf16 ? group_outer_mfma_partial_floats(1, (int)r, (int)di, (int)T, 2) +
+                                group_outer_mfma_partial_floats(1, (int)r, (int)dn, (int)T, 2)
+                          : group_outer_partial_floats(1, (int)r, (int)di, (int)T) +
+                                group_outer_partial_floats(1, (int)r, (int)dn, (int)T);
+  L.partials = take(L.partial_floats * 4);
+  L.padgA = take(padded ? r * di * 4 : 0);
+  L.padgB = take(padded ? dn * r * 4 : 0);
+  L.bwd_end = o > L.fwd_end ? o : L.fwd_end;
+  return L;
+}
+
+int check_dims(const mixlora_linear_dims *D) {
+  if (!D) return MIXLORA_E_NULL;
+  if (D->dtype != MIXLORA_F32 && D->dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
+  if (D->T < 1 || D->d_in < 8 || D->d_out < 8 || D->r < 1 || D->r > 64) return MIXLORA_E_SHAPE;
+  if (D->d_in % 8 || D->d_out % 8) return MIXLORA_E_SHAPE;
+  if ((int64_t)D->T >= (1 << 24)) return MIXLORA_E_SHAPE;
+  return MIXLORA_OK;
+}
+
+int check_q4(const mixlora_linear_dims &D, const mixlora_q4 *q4) {
+  if (!q4 || !q4->codes || !q4->scales) return MIXLORA_E_NULL;
+  if (!mixlora_q4_scale_bytes(D.d_out, D.d_in, q4->group)) return MIXLORA_E_SHAPE;
+  return misaligned(q4->codes) || misaligned(q4->scales) ? MIXLORA_E_ALIGN : MIXLORA_OK;
+}
+
+// p in [0, 1) to sixteenths of a bit of its 16 bits; all of 1 - 2^-17 and above would drop everything
+int make_drop(const mixlora_dropout *d, DropArgs &out) {
+  out = DropArgs{};
+  if (!d) return MIXLORA_OK;
+  if (!(d->p >= 0.f && d->p < 1.f)) return MIXLORA_E_SHAPE;
+  if (d->step && (reinterpret_cast<uintptr_t>(d->step) & 7)) return MIXLORA_E_ALIGN;
+  const uint32_t thr = (uint32_t)std::floor((double)d->p * 65536.0 + 0.5);
+  if (thr >= 65536) return MIXLORA_E_SHAPE;
+  out = DropArgs{thr, (float)(65536.0 / (65536.0 - thr)), (uint32_t)d->seed, (uint32_t)(d->seed >> 32), d->offset, d->step};
+  return MIXLORA_OK;
+}
+
+#define HIP_TRY(expr)                                   \
+  do {                                                  \
+    hipError_t e_ = (expr);                             \
+    if (e_ != hipSuccess) return MIXLORA_E_HIP;         \
+  } while (0)
+
+__global__ void set_offsets_kernel(int32_t *p, int T) {
+  if (threadIdx.x == 0) { p[0] = 0; p[1] = T; }
+}
+
+// fp32 storage: out = D(x), eight elements per thread
+__global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restrict__ x, float *__restrict__ out,
+                                                          int64_t chunks, int per_row, DropArgs drop) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  const uint32_t keep = drop_keep8(drop_key(drop), (uint32_t)(i / per_row), (uint32_t)(i % per_row));
+  Vec8<float> v;
+  v.load(x + i * 8);
+#pragma unroll
+  for (int e = 0; e < 8; e++) v.set(e, keep >> e & 1 ? drop.inv * v.get(e) : 0.f);
+  v.store(out + i * 8);
+}
+
+// out[t, c] = base[t, c] + (c of row t kept ? f * sum_q V[t, q] At[c, q] : 0), rounded once.  Four rows of
+// eight columns per thread.
+constexpr int MLA_ROWS = 4;
+template <typename E>
+__global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *__restrict__ base,
+                                                                 const float *__restrict__ V,
+                                                                 const E *__restrict__ At, E *__restrict__ out,
+                                                                 int T, int C, int r, float f, DropArgs drop) {
+  const int cv = C / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int chunk = (int)(id % cv), c0 = chunk * 8;
+  const int64_t first = id / cv * MLA_ROWS;
+  if (first >= T) return;
+  const int t0 = (int)first;
+  float acc[MLA_ROWS][8];
+#pragma unroll
+  for (int i = 0; i < MLA_ROWS; i++)
+#pragma unroll
+    for (int j = 0; j < 8; j++) acc[i][j] = 0.f;
+  for (int q0 = 0; q0 < r; q0 += 8) {
+    float wv[8][8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      Vec8<E> v;
+      v.load(At + (int64_t)(c0 + j) * r + q0);
+#pragma unroll
+      for (int q = 0; q < 8; q++) wv[j][q] = v.get(q);
+    }
+#pragma unroll
+    for (int i = 0; i < MLA_ROWS; i++) {
+      Vec8<float> pv;
+      pv.load(V + (int64_t)(t0 + i < T ? t0 + i : T - 1) * r + q0);
+#pragma unroll
+      for (int q = 0; q < 8; q++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) acc[i][j] = fmaf(pv.get(q), wv[j][q], acc[i][j]);
+    }
+  }
+  const DropKey key = drop_key(drop);
+#pragma unroll
+  for (int i = 0; i < MLA_ROWS; i++) {
+    if (t0 + i >= T) break;
+    const uint32_t keep = drop_keep8(key, (uint32_t)(t0 + i), (uint32_t)chunk);
+    Vec8<float> b;
+    b.load(base + (int64_t)(t0 + i) * C + c0);
+    Vec8<E> o;
+#pragma unroll
+    for (int j = 0; j < 8; j++) o.set(j, b.get(j) + (keep >> j & 1 ? f * acc[i][j] : 0.f));
+    o.store(out + (int64_t)(t0 + i) * C + c0);
+  }
+}
+template <typename E>
+hipError_t launch_masked_add(const float *base, const float *V, const void *At, void *out, int T, int C, int r, float f,
+                             const DropArgs &drop, hipStream_t st) {
+  const int64_t threads = (int64_t)((T + MLA_ROWS - 1) / MLA_ROWS) * (C / 8);
+  const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
+  hipLaunchKernelGGL(masked_lowrank_add_kernel<E>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, base, V,
+                     (const E *)At, (E *)out, T, C, r, f, drop);
+  if (slot >= 0) prof_mark_end(slot, st, (double)T * C * (4 + sizeof(E)));
+  return hipGetLastError();
+}
+
+GemmProblem problem(int M, int N, void *C, int c_f32, const void *A, const void *B, int K) {
+  GemmProblem p{};
+  p.M = M; p.N = N; p.C = C; p.ldc = N; p.c_f32 = c_f32; p.nseg = 1;
+  p.seg[0].A = A; p.seg[0].lda = K; p.seg[0].B = B; p.seg[0].ldb = K; p.seg[0].K = K;
+  return p;
+}
+
+// bf16: the projection P = D(X) Wq^T [T, r] in all its forms, and the other factor of the rank-r term for
+// cols columns from Wr [cols, r]
+struct Project {
+  const void *X, *Wq, *Wr;
+  int T, K, r, cols, ldT;
+  float s, *P;
+  void *PT, *ext, *ext_B;
+  int32_t *offs;
+};
+hipError_t launch_project(const Project &a, const DropArgs &drop, hipStream_t st) {
+  int e = 0;   // s = m 2^e
+  if (std::isfinite(a.s)) std::frexp(a.s, &e);
+  e = e < -100 ? -100 : e > 100 ? 100 : e;
+  const float m = std::ldexp(a.s, -e);
+  const dim3 grid((a.T + 15) / 16 + ((int64_t)a.cols * (a.r / 8) + 511) / 512), block(512);
+  const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
+#define MIXLORA_PROJECT(NQ_, DROP_)                                                                          \
+  hipLaunchKernelGGL((rank_project_kernel<NQ_, DROP_, true>), grid, block, 0, st, (const bf16_t *)a.X,       \
+                     (const bf16_t *)a.Wq, a.T, a.K, a.r, m, a.P, (bf16_t *)a.PT, a.ldT, (bf16_t *)a.ext,    \
+                     a.offs, (const bf16_t *)a.Wr, a.cols, std::ldexp(1.f, e), (bf16_t *)a.ext_B, drop)
+  if (drop.thr) {
+    if (a.r <= 16) MIXLORA_PROJECT(1, true);
+    else if (a.r <= 32) MIXLORA_PROJECT(2, true);
+    else MIXLORA_PROJECT(4, true);
+  } else {
+    if (a.r <= 16) MIXLORA_PROJECT(1, false);
+    else if (a.r <= 32) MIXLORA_PROJECT(2, false);
+    else MIXLORA_PROJECT(4, false);
+  }
+#undef MIXLORA_PROJECT
+  if (slot >= 0) prof_mark_end(slot, st, 0.0);
+  return hipGetLastError();
+}
+
+// the frozen matrix of a call: one of the two
+struct Frozen {
+  const void *W, *W_T;       // ordinary; W_T may be NULL
+  const mixlora_q4 *q4;
+  Q4Matrix q4_matrix(const mixlora_linear_dims &D) const {
+    return Q4Matrix{(const unsigned char *)q4->codes, (const bf16_t *)q4->scales, D.d_out, D.d_in, q4->group};
+  }
+};
+
+int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B, const DropArgs &drop, const void *x,
+            void *y, char *ws, size_t ws_bytes, hipStream_t st) {
+  const Layout L = make_layout(D, F.q4 != nullptr);
+  if (ws_bytes < L.fwd_end) return MIXLORA_E_WORKSPACE;
+  const int T = D.T, di = D.d_in, dn = D.d_out, dt = D.dtype;
+  if (L.rp != D.r) {   // run on zero-padded banks (they stay in the workspace for the backward)
+    const RelayoutJob jobs[2] = {job_rank_resize(A, ws + L.padA, 1, D.r, L.rp, di, true),
+                                 job_rank_resize(B, ws + L.padB, 1, D.r, L.rp, dn, false)};
+    HIP_TRY(launch_relayout(dt, jobs, 2, st));
+    A = ws + L.padA;
+    B = ws + L.padB;
+  }
+  const int r = L.rp;
+  float *P = (float *)(ws + L.P);
+  const void *W = F.W;
+  if (F.q4) {
+    HIP_TRY(launch_q4_dequantize(F.q4_matrix(D), false, dt, ws + L.W, st));
+    W = ws + L.W;
+  }
+  if (dt == MIXLORA_F32) {
+    const void *xd = x;
+    if (drop.thr) {
+      const int64_t chunks = (int64_t)T * (di / 8);
+      hipLaunchKernelGGL(dropout_f32_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, (const float *)x,
+                         (float *)(ws + L.xd), chunks, di / 8, drop);
+      HIP_TRY(hipGetLastError());
+      xd = ws + L.xd;
+    }
+    const GemmProblem p[2] = {problem(T, dn, y, 0, x, W, di), problem(T, r, P, 1, xd, A, di)};
+    HIP_TRY(launch_gemm(dt, p, 2, st));
+    HIP_TRY(launch_lowrank_add(dt, y, P, B, T, dn, r, D.lora_scale, st));
+    return MIXLORA_OK;
+  }
+  const Project pr{x, A, B, T, di, r, dn, L.ldT, D.lora_scale, P, ws + L.P_T, ws + L.ext, ws + L.ext_B, (int32_t *)(ws + L.offs)};
+  HIP_TRY(launch_project(pr, drop, st));
+  GemmProblem p = problem(T, dn, y, 0, x, W, di);
+  p.seg[1] = GemmSeg{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
+  p.nseg = 2;
+  HIP_TRY(launch_gemm(dt, &p, 1, st, GemmScratch{L.gemm_floats ? (float *)(ws + L.gemm_part) : nullptr, L.gemm_floats}));
+  return MIXLORA_OK;
+}
+
+int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const void *B, const DropArgs &drop, const void *x,
+             const void *dy, char *ws, size_t ws_bytes, void *dx, float *dA, float *dB, hipStream_t st) {
+  const Layout L = make_layout(D, F.q4 != nullptr);
+  if (ws_bytes < L.bwd_end) return MIXLORA_E_WORKSPACE;
+  const int T = D.T, di = D.d_in, dn = D.d_out, dt = D.dtype, r = L.rp;
+  const float s = D.lora_scale;
+  float *dA_user = dA, *dB_user = dB;
+  if (L.rp != D.r) {   // padded banks from the forward pass; padded gradients, cut back at the end
+    A = ws + L.padA;
+    B = ws + L.padB;
+    dA = (float *)(ws + L.padgA);
+    dB = (float *)(ws + L.padgB);
+  }
+  const void *W_T = F.W_T;
+  if (F.q4) {
+    HIP_TRY(launch_q4_dequantize(F.q4_matrix(D), true, dt, ws + L.W_T, st));
+    W_T = ws + L.W_T;
+  } else if (!W_T) {
+    HIP_TRY(launch_transpose(dt, F.W, ws + L.W_T, dn, di, st));
+    W_T = ws + L.W_T;
+  }
+  {
+    const RelayoutJob jobs[2] = {job_bank_T(B, 1, dn, r, ws + L.Bt),     // [d_out, r] -> [r, d_out]
+                                 job_bank_T(A, 1, r, di, ws + L.At)};    // [r, d_in]  -> [d_in, r]
+    HIP_TRY(launch_relayout(dt, jobs, 2, st));
+  }
+  float *V = (float *)(ws + L.V), *P = (float *)(ws + L.P), *part = (float *)(ws + L.partials);
+  const int32_t *offs = (const int32_t *)(ws + L.offs);
+  if (dt == MIXLORA_F32) {
+    const void *xd = x;
+    if (drop.thr) {
+      const int64_t chunks = (int64_t)T * (di / 8);
+      hipLaunchKernelGGL(dropout_f32_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, (const float *)x,
+                         (float *)(ws + L.xd), chunks, di / 8, drop);
+      HIP_TRY(hipGetLastError());
+      xd = ws + L.xd;
+    }
+    hipLaunchKernelGGL(set_offsets_kernel, dim3(1), dim3(64), 0, st, (int32_t *)(ws + L.offs), T);
+    HIP_TRY(hipGetLastError());
+    const GemmProblem p[2] = {problem(T, di, dx, 0, dy, W_T, dn), problem(T, r, V, 1, dy, ws + L.Bt, dn)};
+    HIP_TRY(launch_gemm(dt, p, 2, st));
+    if (drop.thr) HIP_TRY(launch_masked_add<float>((float *)dx, V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
+    else HIP_TRY(launch_lowrank_add(dt, dx, V, ws + L.At, T, di, r, s, st));
+    const GoJob go[2] = {GoJob{offs, nullptr, V, (const float *)xd, dA, 1, r, di, 1, T, 1, s},
+                         GoJob{offs, nullptr, P, (const float *)dy, dB, 1, r, dn, 1, T, 0, s}};
+    HIP_TRY(launch_group_outer(go, 2, part, L.partial_floats, st));
+  } else {
+    const Project pr{dy, ws + L.Bt, ws + L.At, T, dn, r, di, L.ldT, s, V, ws + L.V_T, ws + L.ext, ws + L.ext_B,
+                     (int32_t *)(ws + L.offs)};
+    HIP_TRY(launch_project(pr, DropArgs{}, st));
+    const GemmScratch gs{L.gemm_floats ? (float *)(ws + L.gemm_part) : nullptr, L.gemm_floats};
+    GemmProblem p = problem(T, di, drop.thr ? (void *)(ws + L.dx32) : dx, drop.thr != 0, dy, W_T, dn);
+    if (!drop.thr) {
+      p.seg[1] = GemmSeg{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
+      p.nseg = 2;
+    }
+    HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
+    if (drop.thr)
+      HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
+    const GomJob go[2] = {
+        GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 3, drop},
+        GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, 3, DropArgs{}}};
+    HIP_TRY(launch_group_outer_mfma(go, 2, part, L.partial_floats, st));
+  }
+  if (L.rp != D.r) {
+    const RelayoutJob jobs[2] = {job_rank_resize(dA, dA_user, 1, L.rp, D.r, di, true),
+                                 job_rank_resize(dB, dB_user, 1, L.rp, D.r, dn, false)};
+    HIP_TRY(launch_relayout(MIXLORA_F32, jobs, 2, st));
+  }
+  return MIXLORA_OK;
+}
+
+// arguments common to both kinds of matrix; pointers in order of the call
+int check_pointers(std::initializer_list<const void *> ps) {
+  for (const void *p : ps)
+    if (!p) return MIXLORA_E_NULL;
+  for (const void *p : ps)
+    if (misaligned(p)) return MIXLORA_E_ALIGN;
+  return MIXLORA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_t group, int for_backward) {
+  if (check_dims(dims) != MIXLORA_OK || !mixlora_q4_scale_bytes(dims->d_out, dims->d_in, group)) return 0;
+  const Layout L = make_layout(*dims, true);
+  return for_backward ? L.bwd_end : L.fwd_end;
+}
+
+int mixlora_q4_linear_forward(const mixlora_linear_dims *dims, const mixlora_q4 *q4, const void *A, const void *B,
+                              const mixlora_dropout *dropout, const void *x, void *y, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+  int rc = check_dims(dims);
+  if (rc) return rc;
+  DropArgs drop;
+  if ((rc = check_q4(*dims, q4)) || (rc = make_drop(dropout, drop)) || (rc = check_pointers({A, B, x, y, workspace})))
+    return rc;
+  return forward(*dims, Frozen{nullptr, nullptr, q4}, A, B, drop, x, y, (char *)workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int mixlora_q4_linear_backward(const mixlora_linear_dims *dims, const mixlora_q4 *q4, const void *A, const void *B,
+                               const mixlora_dropout *dropout, const void *x, const void *dy, void *workspace,
+                               size_t workspace_bytes, void *dx, float *dA, float *dB, void *stream) {
+  int rc = check_dims(dims);
+  if (rc) return rc;
+  DropArgs drop;
+  if ((rc = check_q4(*dims, q4)) || (rc = make_drop(dropout, drop)) ||
+      (rc = check_pointers({A, B, x, dy, workspace, dx, dA, dB})))
+    return rc;
+  return backward(*dims, Frozen{nullptr, nullptr, q4}, A, B, drop, x, dy, (char *)workspace, workspace_bytes, dx, dA, dB,
+                  (hipStream_t)stream);
+}
+
+size_t mixlora_lora_dropout_workspace_bytes(const mixlora_linear_dims *dims, int for_backward) {
+  if (check_dims(dims) != MIXLORA_OK) return 0;
+  const Layout L = make_layout(*dims, false);
+  return for_backward ? L.bwd_end : L.fwd_end;
+}
+
+int mixlora_lora_dropout_forward(const mixlora_linear_dims *dims, const void *W, const void *A, const void *B,
+                                 const mixlora_dropout *dropout, const void *x, void *y, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+  int rc = check_dims(dims);
+  if (rc) return rc;
+  DropArgs drop;
+  if ((rc = make_drop(dropout, drop)) || (rc = check_pointers({W, A, B, x, y, workspace}))) return rc;
+  return forward(*dims, Frozen{W, nullptr, nullptr}, A, B, drop, x, y, (char *)workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int mixlora_lora_dropout_backward(const mixlora_linear_dims *dims, const void *W, const void *W_T, const void *A,
+                                  const void *B, const mixlora_dropout *dropout, const void *x, const void *dy,
+                                  void *workspace, size_t workspace_bytes, void *dx, float *dA, float *dB, void *stream) {
+  int rc = check_dims(dims);
+  if (rc) return rc;
+  DropArgs drop;
+  if ((rc = make_drop(dropout, drop)) || (rc = check_pointers({W, A, B, x, dy, workspace, dx, dA, dB}))) return rc;
+  if (W_T && misaligned(W_T)) return MIXLORA_E_ALIGN;
+  return backward(*dims, Frozen{W, W_T, nullptr}, A, B, drop, x, dy, (char *)workspace, workspace_bytes, dx, dA, dB,
+                  (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -398,6 +398,15 @@ hipError_t launch_group_outer(const GoJob *jobs, int njobs, float *partials, siz
                               hipStream_t st);
 size_t group_outer_partial_floats(int G, int r, int C, int rows);
 
+// Dropout of a matrix's elements (csrc/dropout.h has the generator)
+struct DropArgs {
+  uint32_t thr;             // an element is dropped where its 16 bits are below thr; 0: nothing is dropped
+  float inv;                // 65536 / (65536 - thr), the factor of the others
+  uint32_t k0, k1;          // the seed
+  uint64_t offset;
+  const uint64_t *step;     // device, may be NULL: added to offset when a kernel runs
+};
+
 // bf16 MFMA version: smallT is the transposed bf16 factor [r][ldT] (ldT % 8 == 0, readable up to
 // the next multiple of 16 rows past the last group), wide is bf16 with C % 8 == 0.  Up to
 // GOM_MAX_JOBS sums of any shapes go into one launch and one reduction launch; `alike` tells how many
@@ -410,6 +419,8 @@ struct GomJob {
   const int32_t *offs, *pair_of_row;
   int G, r, C, k, rows, ldT, alike, layout_qc;
   float scale;
+  int pieces;      // 3: smallT is [3][r][ldT], three bf16 pieces of an fp32 factor (of every job of a launch); else one
+  DropArgs drop;   // three pieces only: elements of wide that count as zeros (their factor belongs into scale)
 };
 constexpr int GOM_MAX_JOBS = 8;
 hipError_t launch_group_outer_mfma(const GomJob *jobs, int njobs, float *partials, size_t partial_floats,

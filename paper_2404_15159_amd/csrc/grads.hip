@@ -7,6 +7,7 @@
 // token's row).  The sum over rows is split into fixed slices whose partial results are added
 // in a fixed order by a second kernel: no floating-point atomics, bit-reproducible.
 #include "common.h"
+#include "dropout.h"
 
 #include <type_traits>
 
@@ -168,7 +169,10 @@ struct GomBatch {
   int njobs;
 };
 
-template <int NQ>
+// PIECES: smallT holds the factor in that many bf16 pieces ([piece][r][ldT]), whose products with the wide
+// rows go into one sum.  DROP: of a job with drop.thr != 0, the elements of wide that the generator drops
+// count as zeros (wide row = generator row).  Either only adds arithmetic to a step that waits for memory.
+template <int NQ, int PIECES = 1, bool DROP = false>
 __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(GomBatch batch) {
   int ji = 0;
   while (ji + 1 < batch.njobs && batch.x0[ji + 1] <= (int)blockIdx.x) ji++;
@@ -199,15 +203,19 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 #pragma unroll
       for (int i = 0; i < 16; i++) acc[b][j][i] = 0.f;
 
+  DropKey key;
+  if constexpr (DROP) key = drop_key(J.drop);
   auto walk = [&](auto gather) {
   for (int st = st_lo; st < st_hi; st++) {
     const int rbase = base + st * 16 + hi * 8;
-    bf16x8_t bq[NQ];
+    bf16x8_t bq[PIECES][NQ];
 #pragma unroll
-    for (int j = 0; j < NQ; j++) {
-      const int q = j * 32 + l31;
-      bq[j] = *reinterpret_cast<const bf16x8_t *>(smallT + (int64_t)(q < r ? q : 0) * ldT + rbase);
-    }
+    for (int pc = 0; pc < PIECES; pc++)
+#pragma unroll
+      for (int j = 0; j < NQ; j++) {
+        const int q = j * 32 + l31;
+        bq[pc][j] = *reinterpret_cast<const bf16x8_t *>(smallT + (int64_t)(pc * r + (q < r ? q : 0)) * ldT + rbase);
+      }
     // rows read in place are read exactly once per step: a streaming (non-temporal) load keeps them from
     // displacing the gathered rows and partial results other kernels reuse (the sums over the d_ff-wide
     // operands measured 28 % faster); gathered token rows are read by k groups and stay cached
@@ -227,7 +235,16 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 #pragma unroll
       for (int p = 0; p < 8; p++) {
         const int row = rbase + p;
-        bq[j][p] = (qv & (row >= lo) & (row < hi_)) ? bq[j][p] : (bf16_t)0.f;
+#pragma unroll
+        for (int pc = 0; pc < PIECES; pc++)
+          bq[pc][j][p] = (qv & (row >= lo) & (row < hi_)) ? bq[pc][j][p] : (bf16_t)0.f;
+      }
+    }
+    if constexpr (DROP) {
+      if (J.drop.thr) {
+#pragma unroll
+        for (int p = 0; p < 8; p++)
+          wrow[p] = drop_mask8(key, (uint32_t)(rbase + p < nrows ? rbase + p : nrows - 1), (uint32_t)ccol >> 3, wrow[p]);
       }
     }
 #pragma unroll
@@ -236,8 +253,10 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 #pragma unroll
       for (int p = 0; p < 8; p++) fa[p] = wrow[p][b];
 #pragma unroll
-      for (int j = 0; j < NQ; j++)
-        acc[b][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, bq[j], acc[b][j], 0, 0, 0);
+      for (int pc = 0; pc < PIECES; pc++)
+#pragma unroll
+        for (int j = 0; j < NQ; j++)
+          acc[b][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, bq[pc][j], acc[b][j], 0, 0, 0);
     }
   }
   };
@@ -377,8 +396,24 @@ hipError_t launch_group_outer_mfma(const GomJob *jobs, int njobs, float *partial
     n = m > n ? m : n;
   }
   if (used > partial_floats) return hipErrorInvalidValue;
-  if (rmax <= 32) hipLaunchKernelGGL(group_outer_mfma_kernel<1>, dim3(x), dim3(256), 0, st, b);
-  else hipLaunchKernelGGL(group_outer_mfma_kernel<2>, dim3(x), dim3(256), 0, st, b);
+  bool three = false, drop = false;
+  for (int i = 0; i < njobs; i++) {
+    three |= jobs[i].pieces == 3;
+    drop |= jobs[i].drop.thr != 0;
+  }
+  for (int i = 0; i < njobs; i++)   // one instance for all jobs
+    if ((jobs[i].pieces == 3) != three || (drop && !three)) return hipErrorInvalidValue;
+#define MIXLORA_GOM(...) hipLaunchKernelGGL((group_outer_mfma_kernel<__VA_ARGS__>), dim3(x), dim3(256), 0, st, b)
+  if (rmax <= 32) {
+    if (!three) MIXLORA_GOM(1);
+    else if (!drop) MIXLORA_GOM(1, 3);
+    else MIXLORA_GOM(1, 3, true);
+  } else {
+    if (!three) MIXLORA_GOM(2);
+    else if (!drop) MIXLORA_GOM(2, 3);
+    else MIXLORA_GOM(2, 3, true);
+  }
+#undef MIXLORA_GOM
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 0) return e;   // unsplit rows: the kernel wrote the results
   hipLaunchKernelGGL(group_outer_reduce_kernel, dim3((unsigned)((n + 255) / 256), njobs), dim3(256), 0, st, b);

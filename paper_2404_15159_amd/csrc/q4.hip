@@ -1,0 +1,207 @@
+// 4-bit frozen matrices: quantization and back (layout: q4.h).
+#include "q4.h"
+
+namespace mixlora {
+
+typedef bf16_t bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// ---- to codes ---------------------------------------------------------------------------------------
+// scale = the smallest number of six significant bits that is at least most / 6 (most: the group's largest
+// magnitude), so that scale x level has at most eight and is exact in bf16, whichever path widens it; 0 where
+// most < 2^-100, NaN where most >= 2^127 or is not a number.  A code is the nearest level, ties to the even
+// code, found by comparing |w| with (midpoint x scale): those products are exact in fp32, a quotient w / scale
+// would be rounded and could cross a midpoint.
+__device__ __forceinline__ float q4_scale(uint32_t most_bits) {
+  if (most_bits >= 0x7f000000u) return __uint_as_float(0x7fc00000u);
+  if (most_bits < 0x0d800000u) return 0.f;
+  const float most = __uint_as_float(most_bits);
+  constexpr uint32_t LOW = (1u << 18) - 1;
+  uint32_t b = (__float_as_uint(most / 6.f) + LOW) & ~LOW;
+  if (6.f * __uint_as_float(b) < most) b += LOW + 1;   // (the quotient was rounded down onto such a number)
+  return __uint_as_float(b);
+}
+__device__ __forceinline__ uint32_t q4_code(float w, float s) {
+  const float a = fabsf(w);
+  uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) +
+               (a >= 3.5f * s) + (a > 5.f * s);
+  if (s == 0.f) c = 0;
+  return c | (w < 0.f && c ? 8u : 0u);
+}
+
+// Bound by reading W once.  A wavefront owns a tile, a lane eight consecutive inputs of a row four times
+// over; 16 lanes share a row, so a group's largest magnitude is a butterfly over 4, 8 or 16 of them.
+template <typename E>
+__global__ __launch_bounds__(256) void q4_quantize_kernel(const E *__restrict__ W, int n, int K, int group,
+                                                          unsigned char *__restrict__ codes,
+                                                          bf16_t *__restrict__ scales) {
+  const int lane = threadIdx.x & 63;
+  const int64_t kt = q4_col_blocks(K), tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= q4_row_blocks(n) * kt) return;
+  const int row0 = (int)(tile / kt) * Q4_ROWS, k0 = (int)(tile % kt) * Q4_COLS;
+  const int j = lane & 15, k = k0 + 8 * j, per = Q4_COLS / group, lanes = group / 8;
+  Vec8<E> v[4];
+#pragma unroll
+  for (int p = 0; p < 4; p++) {
+    const int row = row0 + p * 4 + (lane >> 4);
+    v[p].load(W + (int64_t)(row < n ? row : n - 1) * K + (k < K ? k : 0));
+  }
+#pragma unroll
+  for (int p = 0; p < 4; p++) {
+    const int i = p * 4 + (lane >> 4);
+    const bool in = row0 + i < n && k < K;   // K is a multiple of 8
+    float w[8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      w[e] = in ? v[p].get(e) : 0.f;
+      const uint32_t b = __float_as_uint(w[e]) & 0x7fffffffu;
+      most = b > most ? b : most;
+    }
+    for (int m = 1; m < lanes; m <<= 1) {
+      const uint32_t o = __shfl_xor(most, m);
+      most = o > most ? o : most;
+    }
+    const float s = q4_scale(most);
+    uint32_t word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) word |= q4_code(w[e], s) << (4 * e);
+    *reinterpret_cast<uint32_t *>(codes + tile * Q4_TILE_BYTES + 16 * (16 * (j & 3) + i) + 4 * (j >> 2)) = word;
+    if (j % lanes == 0) scales[(tile * Q4_ROWS + i) * per + j / lanes] = (bf16_t)s;
+  }
+}
+
+// ---- and back ---------------------------------------------------------------------------------------
+__device__ __forceinline__ void q4_widen8(uint32_t word, float s, float (&v)[8]) {
+  const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 1),
+                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 3);
+  v[0] = s * a[0], v[1] = s * a[1], v[2] = s * b[0], v[3] = s * b[1];
+  v[4] = s * c[0], v[5] = s * c[1], v[6] = s * d[0], v[7] = s * d[1];
+}
+
+// Bound by writing the result.  A wavefront owns a tile.
+template <typename E>
+__global__ __launch_bounds__(256) void q4_dequantize_kernel(Q4Matrix w, E *__restrict__ out) {
+  const int lane = threadIdx.x & 63, i = lane & 15, h = lane >> 4;
+  const int64_t kt = q4_col_blocks(w.K), tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= q4_row_blocks(w.n) * kt) return;
+  const int row = (int)(tile / kt) * Q4_ROWS + i, k0 = (int)(tile % kt) * Q4_COLS, per = Q4_COLS / w.group;
+  const uint4 c = *reinterpret_cast<const uint4 *>(w.codes + tile * Q4_TILE_BYTES + 16 * lane);
+  const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int b = 0; b < 4; b++) {
+    const int k = k0 + 32 * b + 8 * h;
+    const float s = (float)w.scales[(tile * Q4_ROWS + i) * per + 32 * b / w.group];
+    float v[8];
+    q4_widen8(word[b], s, v);
+    Vec8<E> o;
+#pragma unroll
+    for (int e = 0; e < 8; e++) o.set(e, v[e]);
+    if (row < w.n && k < w.K) o.store(out + (int64_t)row * w.K + k);
+  }
+}
+
+// Transposed: a workgroup widens four tiles of 64 rows, whose columns are then rows of the result, through
+// LDS (pitch 64 + 8 elements).
+template <typename E>
+__global__ __launch_bounds__(256) void q4_dequantize_T_kernel(Q4Matrix w, E *__restrict__ out) {
+  constexpr int R = 4 * Q4_ROWS, PITCH = R + 8;
+  __shared__ __align__(16) E buf[Q4_COLS][PITCH];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, h = lane >> 4;
+  const int64_t kt = q4_col_blocks(w.K), nt = q4_row_blocks(w.n), groups = (nt + 3) / 4;
+  const int64_t at = blockIdx.x, cb = at / groups, rb = (at % groups) * 4 + wave;
+  const int64_t tile = (rb < nt ? rb : nt - 1) * kt + cb;
+  const int k0 = (int)cb * Q4_COLS, row0 = (int)(at % groups) * R, per = Q4_COLS / w.group;
+  const uint4 c = *reinterpret_cast<const uint4 *>(w.codes + tile * Q4_TILE_BYTES + 16 * lane);
+  const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int b = 0; b < 4; b++) {
+    const float s = (float)w.scales[(tile * Q4_ROWS + i) * per + 32 * b / w.group];
+    float v[8];
+    q4_widen8(word[b], s, v);
+#pragma unroll
+    for (int e = 0; e < 8; e++) buf[32 * b + 8 * h + e][wave * Q4_ROWS + i] = from_f32<E>(v[e]);
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < Q4_COLS * (R / 8); p += 256) {
+    const int k = p / (R / 8), n = p % (R / 8) * 8;
+    if (k0 + k < w.K && row0 + n < w.n) {   // n is a multiple of 8
+      Vec8<E> o;
+      o.load(&buf[k][n]);
+      o.store(out + (int64_t)(k0 + k) * w.n + row0 + n);
+    }
+  }
+}
+
+hipError_t launch_q4_dequantize(const Q4Matrix &w, bool transposed, int dtype, void *out, hipStream_t st) {
+  const int64_t tiles = q4_row_blocks(w.n) * q4_col_blocks(w.K);
+  const dim3 grid((unsigned)(transposed ? (q4_row_blocks(w.n) + 3) / 4 * q4_col_blocks(w.K) : (tiles + 3) / 4)), block(256);
+  const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
+  if (transposed && dtype == MIXLORA_BF16)
+    hipLaunchKernelGGL(q4_dequantize_T_kernel<bf16_t>, grid, block, 0, st, w, (bf16_t *)out);
+  else if (transposed)
+    hipLaunchKernelGGL(q4_dequantize_T_kernel<float>, grid, block, 0, st, w, (float *)out);
+  else if (dtype == MIXLORA_BF16)
+    hipLaunchKernelGGL(q4_dequantize_kernel<bf16_t>, grid, block, 0, st, w, (bf16_t *)out);
+  else
+    hipLaunchKernelGGL(q4_dequantize_kernel<float>, grid, block, 0, st, w, (float *)out);
+  if (slot >= 0) prof_mark_end(slot, st, (double)w.n * w.K * (dtype == MIXLORA_BF16 ? 2.5 : 4.5));
+  return hipGetLastError();
+}
+
+}  // namespace mixlora
+
+using namespace mixlora;
+
+namespace {
+inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+int check_matrix(int32_t d_out, int32_t d_in, int32_t group) {
+  if (d_out < 8 || d_in < 8 || d_out % 8 || d_in % 8 || !q4_group_ok(group)) return MIXLORA_E_SHAPE;
+  if (q4_row_blocks(d_out) * q4_col_blocks(d_in) >= (1ll << 31)) return MIXLORA_E_SHAPE;   // a tile per wavefront
+  return MIXLORA_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t mixlora_q4_code_bytes(int32_t d_out, int32_t d_in) {
+  return check_matrix(d_out, d_in, 128) ? 0 : q4_code_bytes(d_out, d_in);
+}
+
+size_t mixlora_q4_scale_bytes(int32_t d_out, int32_t d_in, int32_t group) {
+  return check_matrix(d_out, d_in, group) ? 0 : q4_scale_bytes(d_out, d_in, group);
+}
+
+int mixlora_q4_quantize(const void *W, int32_t dtype, int32_t d_out, int32_t d_in, const mixlora_q4 *q4,
+                        void *stream) {
+  if (!q4 || !W || !q4->codes || !q4->scales) return MIXLORA_E_NULL;
+  if (dtype != MIXLORA_F32 && dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
+  const int rc = check_matrix(d_out, d_in, q4->group);
+  if (rc) return rc;
+  if (misaligned(W) || misaligned(q4->codes) || misaligned(q4->scales)) return MIXLORA_E_ALIGN;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const int64_t tiles = q4_row_blocks(d_out) * q4_col_blocks(d_in);
+  const dim3 grid((unsigned)((tiles + 3) / 4)), block(256);
+  if (dtype == MIXLORA_BF16)
+    hipLaunchKernelGGL(q4_quantize_kernel<bf16_t>, grid, block, 0, st, (const bf16_t *)W, d_out, d_in, q4->group,
+                       (unsigned char *)q4->codes, (bf16_t *)q4->scales);
+  else
+    hipLaunchKernelGGL(q4_quantize_kernel<float>, grid, block, 0, st, (const float *)W, d_out, d_in, q4->group,
+                       (unsigned char *)q4->codes, (bf16_t *)q4->scales);
+  return hipGetLastError() == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
+}
+
+int mixlora_q4_dequantize(const mixlora_q4 *q4, int32_t d_out, int32_t d_in, int32_t transposed, void *W,
+                          int32_t dtype, void *stream) {
+  if (!q4 || !W || !q4->codes || !q4->scales) return MIXLORA_E_NULL;
+  if (dtype != MIXLORA_F32 && dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
+  const int rc = check_matrix(d_out, d_in, q4->group);
+  if (rc) return rc;
+  if (transposed != 0 && transposed != 1) return MIXLORA_E_SHAPE;
+  if (misaligned(W) || misaligned(q4->codes) || misaligned(q4->scales)) return MIXLORA_E_ALIGN;
+  const Q4Matrix m{(const unsigned char *)q4->codes, (const bf16_t *)q4->scales, d_out, d_in, q4->group};
+  return launch_q4_dequantize(m, transposed != 0, dtype, W, reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+             ? MIXLORA_OK : MIXLORA_E_HIP;
+}
+
+}  // extern "C"

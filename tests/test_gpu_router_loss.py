@@ -1,0 +1,153 @@
+"""Routing with its losses over padded batches on the GPU against the float64 definition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as orc
+from paper_2404_15159_amd import binding as B
+from test_gpu_q4 import CODE, DEV, Guarded, TD, dev, rounded
+
+pytestmark = pytest.mark.gpu
+MODE = {"top1": B.AUX_TOP1, "topk": B.AUX_TOPK}
+
+
+def run(z, mask, k, mode, dtype, dw, gb=1.0, gz=1.0, bc=0.01, zc=0.001):
+    T, N = z.shape
+    dims = B.RouterDims(T, N, k, bc, zc, MODE[mode], CODE[dtype])
+    zt = dev(z, dtype)
+    mt = None if mask is None else torch.from_numpy(np.asarray(mask, np.uint8)).to(DEV)
+    n = B.mixlora_router_loss_workspace_bytes(dims)
+    ws = Guarded((n,), torch.uint8, 205)
+    o = dict(loss=Guarded((3,), torch.float32), counts=Guarded((N,), torch.int32, 77),
+             topk_idx=Guarded((T, k), torch.int32, 77), topk_w=Guarded((T, k), torch.float32),
+             dlogits=Guarded((T, N), TD[dtype]))
+    dwt = None if dw is None else dev(dw, "f32")
+    B.mixlora_router_loss_forward(dims, zt, mt, o["loss"].t, o["counts"].t, o["topk_idx"].t, o["topk_w"].t, ws.t, n)
+    B.mixlora_router_loss_backward(dims, zt, mt, o["topk_idx"].t if dw is not None else None, dwt, gb, gz, ws.t, n,
+                                   o["dlogits"].t)
+    torch.cuda.synchronize()
+    ws.numpy()
+    return {k: v.numpy() for k, v in o.items()}
+
+
+def compare(got, want, N, dtype):
+    for n in ("counts", "topk_idx"):
+        assert np.array_equal(got[n], want[n]), n
+    # exp and log are good to two steps, a row's sums have N terms; the losses' sums are over tokens in
+    # fp32 by wavefronts (8 steps of a butterfly and 4 partial sums), then in double
+    e = (N + 40) * 2.0 ** -23
+    assert np.all(np.abs(got["topk_w"] - want["topk_w"]) <= e * np.abs(want["topk_w"]) + 1e-37)
+    assert np.all(np.abs(got["loss"] - want["loss"]) <= e * np.abs(want["loss"]) + 1e-37), (got["loss"], want["loss"])
+
+
+def bound_dlogits(z, mask, k, mode, dw, gb, gz, bc, zc, want, dtype):
+    """magnitudes of the terms that a gradient is a sum of"""
+    T, N = z.shape
+    n = max(1, int(np.sum(mask)) if mask is not None else T)
+    terms = np.zeros((T, N))
+    for t in range(T):
+        if mask is not None and not mask[t]:
+            continue
+        with np.errstate(invalid="ignore"):
+            ez = np.exp(z[t].astype(np.float64) - z[t].max())
+            p = ez / ez.sum()
+            lse = z[t].max() + np.log(ez.sum())
+        terms[t] = p * (abs(gb) * bc * N / n * 2 + abs(gz) * zc * 2 / n * (abs(lse) + abs(z[t].max()) + 1))
+        if dw is not None:
+            i = want["topk_idx"][t]
+            w = want["topk_w"][t]
+            terms[t, i] += w * (np.abs(dw[t]) + (w * np.abs(dw[t])).sum())
+    step = 2.0 ** -8 if dtype == "bf16" else 0.0
+    return step * np.abs(want["dlogits"]) + (N + 40) * 2.0 ** -23 * terms + 1e-37
+
+
+CASES = [
+    # T, N, k, mode, dtype, share kept by the mask (None: no mask), d_topk_w
+    (1, 1, 1, "top1", "f32", None, True),
+    (1, 8, 2, "top1", "f32", 1.0, True),
+    (7, 4, 1, "topk", "bf16", 0.5, True),
+    (63, 7, 3, "topk", "f32", 0.5, False),
+    (64, 8, 2, "top1", "bf16", None, True),
+    (255, 16, 2, "top1", "f32", 0.7, True),
+    (256, 16, 16, "topk", "f32", 0.7, True),
+    (257, 17, 2, "top1", "f32", 0.3, True),
+    (300, 33, 5, "topk", "bf16", 0.9, True),
+    (513, 64, 6, "top1", "f32", 0.5, True),
+    (1000, 64, 64, "topk", "f32", None, True),
+    (4099, 8, 2, "top1", "f32", 0.7, True),
+    (300, 8, 2, "top1", "f32", 0.0, True),
+]
+
+
+@pytest.mark.parametrize("T,N,k,mode,dtype,keep,with_dw", CASES)
+def test_router(T, N, k, mode, dtype, keep, with_dw):
+    print(f"case router T={T} N={N} k={k} {mode} {dtype} keep={keep}", flush=True)
+    rng = np.random.default_rng(T + N)
+    z = rounded(rng.normal(0, 1.5, (T, N)), dtype)      # bf16 logits tie often
+    mask = None if keep is None else rng.random(T) < keep
+    dw = rng.normal(size=(T, k)).astype(np.float32) if with_dw else None
+    got = run(z, mask, k, mode, dtype, dw, 0.7, 1.3)
+    want = orc.router(z, mask, k, mode, 0.01, 0.001, dw, 0.7, 1.3)
+    compare(got, want, N, dtype)
+    b = bound_dlogits(z, mask, k, mode, dw, 0.7, 1.3, 0.01, 0.001, want, dtype)
+    off = np.abs(got["dlogits"] - want["dlogits"])
+    print(f"  dlogits: worst {np.max(off / b):.3f} of its bound", flush=True)
+    assert np.all(off <= b)
+
+
+def test_ties_and_extremes():
+    """Equal logits go to the lower index; -inf is an expert that is never first; the type's lowest value and large
+    logits stay finite; NaN in a token that does not count reaches nothing, in one that does it reaches its own row."""
+    low = float(np.finfo(np.float32).min)
+    z = np.zeros((9, 5), np.float32)
+    z[1] = [-np.inf, 0, -np.inf, 0, -np.inf]
+    z[2] = [low, 1, low, low, low]
+    z[3] = [300, 299, -300, 300, 0]
+    z[4] = np.nan
+    z[5] = np.inf
+    z[6] = [88, 88.5, 89, 88, 88]
+    z[7] = [-200, -201, -200, -205, -202]
+    mask = np.array([1, 1, 1, 1, 0, 0, 1, 1, 1])
+    dw = np.ones((9, 2), np.float32) * [[1, -2]]
+    got = run(z, mask, 2, "top1", "f32", dw.astype(np.float32))
+    with np.errstate(invalid="ignore"):
+        want = orc.router(z, mask, 2, "top1", 0.01, 0.001, dw)
+    compare(got, want, 5, "f32")
+    assert np.array_equal(got["topk_idx"][:4], [[0, 1], [1, 3], [1, 0], [0, 3]])
+    assert np.isfinite(got["dlogits"]).all() and not got["dlogits"][4:6].any()
+    mask[4] = 1
+    got = run(z, mask, 2, "top1", "f32", dw.astype(np.float32))
+    assert np.isnan(got["loss"][0]) and np.array_equal(got["topk_idx"][4], [0, 1])
+    assert np.isnan(got["dlogits"][4]).all() and np.array_equal(got["topk_idx"][:4], [[0, 1], [1, 3], [1, 0], [0, 3]])
+
+
+def test_reruns_and_graph():
+    rng = np.random.default_rng(9)
+    T, N, k = 3000, 16, 2
+    dims = B.RouterDims(T, N, k, 0.01, 0.001, B.AUX_TOP1, B.F32)
+    z, mask = dev(rng.normal(size=(T, N)), "f32"), torch.from_numpy((rng.random(T) < 0.6).astype(np.uint8)).to(DEV)
+    dw = dev(rng.normal(size=(T, k)), "f32")
+    n = B.mixlora_router_loss_workspace_bytes(dims)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    o = [torch.empty(s, dtype=d, device=DEV) for s, d in ((3, torch.float32), (N, torch.int32), ((T, k), torch.int32),
+                                                          ((T, k), torch.float32), ((T, N), torch.float32))]
+
+    def both():
+        B.mixlora_router_loss_forward(dims, z, mask, o[0], o[1], o[2], o[3], ws, n)
+        B.mixlora_router_loss_backward(dims, z, mask, o[2], dw, 1.0, 1.0, ws, n, o[4])
+
+    both()
+    first = [v.clone() for v in o]
+    both()
+    assert all(torch.equal(a, b) for a, b in zip(first, o))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for i in range(3):
+        z.copy_(torch.randn_like(z))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in o]
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, o)), i
