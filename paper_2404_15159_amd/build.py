@@ -28,7 +28,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmixlora.so")
 SOURCES = ("gemm.hip", "router.hip", "elementwise.hip", "grads.hip", "fused.hip", "fused_pg.hip", "fused_few.hip",
            "tail.hip",
-           "probe.hip", "linear.hip", "adapter_linear.hip", "q4.hip", "router_loss.hip", "optim.hip", "dora.hip", "prof.hip", "api.hip")
+           "probe.hip", "linear.hip", "adapter_linear.hip", "q4.hip", "q4_few.hip", "router_loss.hip", "optim.hip", "dora.hip", "prof.hip", "api.hip")
 
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

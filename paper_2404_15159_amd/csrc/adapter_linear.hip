@@ -5,9 +5,11 @@
 // product as an extra K segment, in three bf16 pieces that hold all of its 24 bits, in the backward too
 // where there is no dropout; with dropout the product is made in fp32 and the masked term is added where it
 // is rounded, so that a result is rounded once.  The gradient sums take the rank-r factor in three pieces as
-// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h).
+// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h), but for the forward of up to
+// 128 rows, which multiplies with the codes (q4_few.hip).
 #include "common.h"
 #include "q4.h"
+#include "q4_few.h"
 #include "rank_project.h"
 
 #include <cmath>
@@ -27,7 +29,8 @@ struct Layout {
   size_t ext, ext_B, gemm_part, xd;       // scratch of either direction
   size_t W, fwd_end;
   size_t W_T, Bt, At, V, V_T, dx32, partials, padgA, padgB, bwd_end;
-  size_t gemm_floats, partial_floats;
+  size_t few;                             // partial sums of the few-rows product
+  size_t gemm_floats, partial_floats, few_floats;
 };
 
 // q4: room for the widened matrix.  The scratch of the two directions overlaps.
@@ -54,7 +57,10 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   }
   L.xd = take(bf16 ? 0 : T * di * E);
   const size_t scratch = o;
-  L.W = take(q4 ? di * dn * E : 0);
+  // up to 128 rows in bf16 multiply with the codes themselves
+  L.few_floats = q4 && bf16 ? q4_few_scratch_floats((int)dn, (int)di, (int)T, (int)r) : 0;
+  L.few = take(L.few_floats * 4);
+  L.W = take(q4 && !L.few_floats ? di * dn * E : 0);
   L.fwd_end = o;
   o = scratch;
   L.W_T = take(di * dn * E);
@@ -251,6 +257,11 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
   const int r = L.rp;
   float *P = (float *)(ws + L.P);
   const void *W = F.W;
+  if (L.few_floats) {   // (the backward makes the projection itself)
+    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.lora_scale, (bf16_t *)y};
+    HIP_TRY(launch_q4_few(F.q4_matrix(D), a, drop, (float *)(ws + L.few), L.few_floats, st));
+    return MIXLORA_OK;
+  }
   if (F.q4) {
     HIP_TRY(launch_q4_dequantize(F.q4_matrix(D), false, dt, ws + L.W, st));
     W = ws + L.W;
@@ -325,6 +336,10 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
                          GoJob{offs, nullptr, P, (const float *)dy, dB, 1, r, dn, 1, T, 0, s}};
     HIP_TRY(launch_group_outer(go, 2, part, L.partial_floats, st));
   } else {
+    if (L.few_floats) {   // the forward has not kept the projection
+      const Project px{x, A, B, T, di, r, 0, L.ldT, s, P, ws + L.P_T, ws + L.ext, ws + L.ext_B, (int32_t *)(ws + L.offs)};
+      HIP_TRY(launch_project(px, drop, st));
+    }
     const Project pr{dy, ws + L.Bt, ws + L.At, T, dn, r, di, L.ldT, s, V, ws + L.V_T, ws + L.ext, ws + L.ext_B,
                      (int32_t *)(ws + L.offs)};
     HIP_TRY(launch_project(pr, DropArgs{}, st));

@@ -1,0 +1,17 @@
+// Few rows through a LoRA linear on a 4-bit matrix (csrc/q4_few.hip)
+#pragma once
+#include "q4.h"
+
+namespace mixlora {
+
+constexpr int Q4_FEW_ROWS = 128;
+struct Q4Few {
+  const bf16_t *x, *A, *B;   // [T, K], [r, K], [n, r]; r a multiple of 8
+  int T, r;
+  float s;
+  bf16_t *y;                 // [T, n]
+};
+size_t q4_few_scratch_floats(int n, int K, int T, int r);
+hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop, float *scratch, size_t floats, hipStream_t st);
+
+}  // namespace mixlora
