@@ -37,6 +37,13 @@ template <> __device__ __forceinline__ void q4_load_scales<4>(const bf16_t *p, f
   s[2] = __uint_as_float(v.y << 16), s[3] = __uint_as_float(v.y & 0xffff0000u);
 }
 
+// a lane's codes and scales of a tile (uniform over the wavefront)
+template <int PER>
+__device__ __forceinline__ void q4_load(const Q4Matrix &w, int64_t tile, int lane, uint4 &c, float (&s)[PER]) {
+  c = *reinterpret_cast<const uint4 *>(w.codes + tile * Q4_TILE_BYTES + (uint32_t)lane * 16u);
+  q4_load_scales<PER>(w.scales + tile * (Q4_ROWS * PER) + (uint32_t)(lane & 15) * PER, s);
+}
+
 // acc += (sums of x times level over each group of the tile) x scale; MT blocks of 16 rows
 template <int MT, int PER>
 __device__ __forceinline__ void q4_tile(const bf16x8_t (&fx)[MT][4], const uint4 &c, const float (&s)[PER],
@@ -61,36 +68,84 @@ __device__ __forceinline__ void q4_tile(const bf16x8_t (&fx)[MT][4], const uint4
   }
 }
 
-// 32 inputs per step of a row block's operand, zeros past K
-__device__ __forceinline__ void load_rows(const bf16_t *row, int k0, int hi, int K, bf16x8_t (&f)[4]) {
+// Rows of a bf16 matrix as MFMA operands: 16 rows x 128 inputs, 4 KB.  In the operand's own layout neighbouring
+// lanes hold different rows, and a load of it is 64 requests of 16 bytes (the rank-r rows of one token's product
+// cost 5.1 us that way at 16 x 4096, 1.5 this way).  So they are loaded 256 bytes of a row at a time and change
+// lanes in a piece of LDS that belongs to the wavefront alone, its 16-byte chunks in an order that leaves no two
+// lanes of a group in one bank.
+constexpr int STAGE_BYTES = 4096;
+struct RowOffsets {
+  uint32_t off[4];   // bytes; K < 2^23
+  // rows first .. first + 15 of `rows` (clamped: what is past the last one is not used)
+  __device__ __forceinline__ RowOffsets(int first, int rows, int K, int lane) {
 #pragma unroll
-  for (int st = 0; st < 4; st++) {
-    const int k = k0 + st * 32 + hi * 8;
-    f[st] = *reinterpret_cast<const bf16x8_t *>(row + (k < K ? k : 0));
+    for (int p = 0; p < 4; p++) {
+      const int row = first + p * 4 + (lane >> 4);
+      off[p] = (uint32_t)(row < rows ? row : rows - 1) * (uint32_t)K * 2u + (lane & 15) * 16;
+    }
+  }
+};
+// (kb is uniform over the wavefront; past K, in the last tile, the tile's first chunk is read instead)
+__device__ __forceinline__ void rows_load(const bf16_t *base, const RowOffsets &o, int kb, int K, int lane, bf16x8_t (&v)[4]) {
+  const unsigned char *p = reinterpret_cast<const unsigned char *>(base) + (int64_t)kb * (Q4_COLS * 2);
+  if ((kb + 1) * Q4_COLS <= K) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = *reinterpret_cast<const bf16x8_t *>(p + o.off[i]);
+  } else {
+    const uint32_t back = kb * Q4_COLS + (lane & 15) * 8 < K ? 0u : (lane & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = *reinterpret_cast<const bf16x8_t *>(p + (o.off[i] - back));
   }
 }
-__device__ __forceinline__ void zero_past(int k0, int hi, int K, bf16x8_t (&f)[4]) {
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bf16x8_t zero_unless(bool in, bf16x8_t v) {
+  u32x4_t w = __builtin_bit_cast(u32x4_t, v);
+#pragma unroll
+  for (int e = 0; e < 4; e++) w[e] = in ? w[e] : 0u;
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+__device__ __forceinline__ void rows_to_lds(unsigned char *lds, bf16x8_t (&v)[4], int kb, int K, int lane) {
+  if ((kb + 1) * Q4_COLS > K) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = zero_unless(kb * Q4_COLS + (lane & 15) * 8 < K, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int row = i * 4 + (lane >> 4);
+    *reinterpret_cast<bf16x8_t *>(lds + row * 256 + ((lane ^ row) & 15) * 16) = v[i];
+  }
+}
+__device__ __forceinline__ void rows_from_lds(const unsigned char *lds, int lane, bf16x8_t (&f)[4]) {
+  const int l15 = lane & 15, hi = lane >> 4;
 #pragma unroll
   for (int st = 0; st < 4; st++)
-    if (k0 + st * 32 + hi * 8 >= K) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) f[st][e] = (bf16_t)0.f;
-    }
+    f[st] = *reinterpret_cast<const bf16x8_t *>(lds + l15 * 256 + (((st * 4 + hi) ^ l15) & 15) * 16);
+}
+// between the two: the wavefront's LDS accesses keep their order (the hardware takes them in order)
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// ---- up to 16 rows, rank up to 16, no dropout: one launch ---------------------------------------------
+// ---- up to 64 rows, rank up to 16, no dropout: one launch ---------------------------------------------
 // A workgroup owns NT tiles' rows (16 NT columns of y) over the whole contraction, its eight wavefronts every
-// eighth tile of it, two tiles ahead of the one in use.  Every workgroup makes the projection x A^T itself (128
-// KB of A at 16 x 4096, out of L2): that costs less than a launch in front of this one.
-template <int NT, int PER>
+// eighth tile of it; MT blocks of 16 rows of x.  Every workgroup makes the projection x A^T itself (128 KB of A at
+// 16 x 4096, out of L2): that costs less than a launch in front of this one.  Nothing is requested ahead within a
+// wavefront: with the registers that takes, fewer of them fit, and one token 4096 -> 4096 took 6.6 instead of 5.4 us.
+// ONE: a single row of x, which every lane can read for itself.
+template <int NT, int MT, int PER, bool ONE>
 __global__ __launch_bounds__(512) void q4_few_kernel(Q4Matrix w, Q4Few a) {
-  constexpr int WAVES = 8, UN = 2;
-  __shared__ float red[WAVES][NT + 1][64][4];
-  __shared__ float sp[16][17];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, hi = lane >> 4;
+  static_assert(!ONE || MT == 1, "one row is one block");
+  constexpr int WAVES = 8;
+  // staging of A, then of x, wavefront by wavefront; sums [8][NT + 1][MT][64][4] (the last: of the projection), and
+  // the projection itself
+  extern __shared__ __align__(16) unsigned char smem[];
+  auto red = reinterpret_cast<float(*)[NT + 1][MT][64][4]>(smem);
+  auto sp = reinterpret_cast<float(*)[17]>(smem + WAVES * (NT + 1) * MT * 1024);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 4;
   const int rb0 = blockIdx.x * NT, row_blocks = (int)q4_row_blocks(w.n), kbs = (int)q4_col_blocks(w.K);
   const int T = a.T, r = a.r, K = w.K;
-  // what the end needs of B: column col of tile i for token tok
+  // what the end needs of B: column col of tile i for tokens tok, tok + 16, ..
   const int col = tid & 15, tok = (tid >> 4) & 15, half = tid >> 8;
   constexpr int OUT = (NT + 1) / 2;
   bf16x8_t bq[OUT][2];
@@ -101,85 +156,129 @@ __global__ __launch_bounds__(512) void q4_few_kernel(Q4Matrix w, Q4Few a) {
     for (int h = 0; h < 2; h++)
       bq[o][h] = *reinterpret_cast<const bf16x8_t *>(a.B + (int64_t)(n < w.n ? n : 0) * r + (8 * h < r ? 8 * h : 0));
   }
-  const bf16_t *xr = a.x + (int64_t)(l15 < T ? l15 : T - 1) * K;
-  const bf16_t *ar = a.A + (int64_t)(l15 < r ? l15 : r - 1) * K;
-  const unsigned char *cr[NT];
-  const bf16_t *sr[NT];
+  unsigned char *stage = smem + wave * MT * STAGE_BYTES;
+  int64_t first[NT];   // tiles in front of each row block
 #pragma unroll
-  for (int i = 0; i < NT; i++) {
-    const int64_t first = (int64_t)(rb0 + i < row_blocks ? rb0 + i : row_blocks - 1) * kbs;
-    cr[i] = w.codes + first * Q4_TILE_BYTES + 16 * lane;
-    sr[i] = w.scales + (first * Q4_ROWS + l15) * PER;
+  for (int i = 0; i < NT; i++) first[i] = (int64_t)(rb0 + i < row_blocks ? rb0 + i : row_blocks - 1) * kbs;
+  f32x4_t acc[NT][MT], accp[MT];
+#pragma unroll
+  for (int m = 0; m < MT; m++) {
+    accp[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; i++) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  f32x4_t acc[NT][1], accp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < NT; i++) acc[i][0] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  struct Block {
-    bf16x8_t fx[1][4], fa[4];
+  const RowOffsets oa(0, r, K, lane);
+  for (int kb = wave; kb < kbs; kb += WAVES) {
     uint4 c[NT];
     float s[NT][PER];
-  };
-  auto load = [&](int kb, Block &b) {
-    const int kc = kb < kbs ? kb : kbs - 1;
+    bf16x8_t va[4], vx[MT][4], fa[4], fx[MT][4];
+    rows_load(a.A, oa, kb, K, lane, va);
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-      b.c[i] = *reinterpret_cast<const uint4 *>(cr[i] + (int64_t)kc * Q4_TILE_BYTES);
-      q4_load_scales<PER>(sr[i] + (int64_t)kc * Q4_ROWS * PER, b.s[i]);
+    for (int i = 0; i < NT; i++) q4_load<PER>(w, first[i] + kb, lane, c[i], s[i]);
+    if constexpr (ONE) {
+#pragma unroll
+      for (int st = 0; st < 4; st++) {
+        const int k = st * 32 + hi * 8;
+        fx[0][st] = *reinterpret_cast<const bf16x8_t *>(
+            a.x + (int64_t)kb * Q4_COLS + (uint32_t)((kb + 1) * Q4_COLS <= K || kb * Q4_COLS + k < K ? k : 0));
+      }
+      if ((kb + 1) * Q4_COLS > K) {
+#pragma unroll
+        for (int st = 0; st < 4; st++) fx[0][st] = zero_unless(kb * Q4_COLS + st * 32 + hi * 8 < K, fx[0][st]);
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < MT; m++) rows_load(a.x, RowOffsets(m * 16, T, K, lane), kb, K, lane, vx[m]);
     }
-    load_rows(xr, kc * Q4_COLS, hi, K, b.fx[0]);
-    load_rows(ar, kc * Q4_COLS, hi, K, b.fa);
-  };
-  auto use = [&](int kb, Block &b) {
-    if (kb >= kbs) return;   // (wavefront-uniform)
-    if (kb == kbs - 1) {
-      zero_past(kb * Q4_COLS, hi, K, b.fx[0]);
-      zero_past(kb * Q4_COLS, hi, K, b.fa);
+    wave_order();
+    rows_to_lds(stage, va, kb, K, lane);
+    wave_order();
+    rows_from_lds(stage, lane, fa);
+    if constexpr (!ONE) {
+      wave_order();
+#pragma unroll
+      for (int m = 0; m < MT; m++) rows_to_lds(stage + m * STAGE_BYTES, vx[m], kb, K, lane);
+      wave_order();
+#pragma unroll
+      for (int m = 0; m < MT; m++) rows_from_lds(stage + m * STAGE_BYTES, lane, fx[m]);
     }
 #pragma unroll
-    for (int st = 0; st < 4; st++) accp = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.fx[0][st], b.fa[st], accp, 0, 0, 0);
+    for (int st = 0; st < 4; st++)
 #pragma unroll
-    for (int i = 0; i < NT; i++) q4_tile<1, PER>(b.fx, b.c[i], b.s[i], acc[i]);
-  };
-  Block cur[UN], nxt[UN];
+      for (int m = 0; m < MT; m++) accp[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[m][st], fa[st], accp[m], 0, 0, 0);
 #pragma unroll
-  for (int u = 0; u < UN; u++) load(wave + u * WAVES, cur[u]);
-  for (int kb = wave; kb < kbs; kb += UN * WAVES) {
-#pragma unroll
-    for (int u = 0; u < UN; u++) load(kb + (UN + u) * WAVES, nxt[u]);
-#pragma unroll
-    for (int u = 0; u < UN; u++) use(kb + u * WAVES, cur[u]);
-#pragma unroll
-    for (int u = 0; u < UN; u++) cur[u] = nxt[u];
+    for (int i = 0; i < NT; i++) q4_tile<MT, PER>(fx, c[i], s[i], acc[i]);
   }
+  __syncthreads();   // the staging is behind everybody
   // lane (l15, hi), register u: row 4 hi + u, column l15
 #pragma unroll
-  for (int i = 0; i < NT; i++) *reinterpret_cast<f32x4_t *>(red[wave][i][lane]) = acc[i][0];
-  *reinterpret_cast<f32x4_t *>(red[wave][NT][lane]) = accp;
+  for (int m = 0; m < MT; m++) {
+#pragma unroll
+    for (int i = 0; i < NT; i++) *reinterpret_cast<f32x4_t *>(red[wave][i][m][lane]) = acc[i][m];
+    *reinterpret_cast<f32x4_t *>(red[wave][NT][m][lane]) = accp[m];
+  }
   __syncthreads();
   const int ln = (tok >> 2) * 16 + col, u = tok & 3;
-  if (tid < 256) {
-    float v = red[0][NT][ln][u];
 #pragma unroll
-    for (int q = 1; q < WAVES; q++) v += red[q][NT][ln][u];
-    sp[tok][col] = col < r ? v : 0.f;
+  for (int m = 0; m < MT; m++) {
+    if ((m & 1) != half) continue;   // the halves of the workgroup share the row blocks
+    float v = red[0][NT][m][ln][u];
+#pragma unroll
+    for (int q = 1; q < WAVES; q++) v += red[q][NT][m][ln][u];
+    sp[m * 16 + tok][col] = col < r ? v : 0.f;
   }
   __syncthreads();
-  if (tok >= T) return;
 #pragma unroll
-  for (int o = 0; o < OUT; o++) {
-    const int i = half + 2 * o, n = (rb0 + i) * 16 + col;
-    if (i >= NT || n >= w.n) continue;
-    float v = red[0][i][ln][u], p = 0.f;
+  for (int m = 0; m < MT; m++) {
+    const int t = m * 16 + tok;
+    if (t >= T) break;
 #pragma unroll
-    for (int q = 1; q < WAVES; q++) v += red[q][i][ln][u];
+    for (int o = 0; o < OUT; o++) {
+      const int i = half + 2 * o, n = (rb0 + i) * 16 + col;
+      if (i >= NT || n >= w.n) continue;
+      float v = red[0][i][m][ln][u], p = 0.f;
 #pragma unroll
-    for (int q = 0; q < 8; q++) p = fmaf(sp[tok][q], (float)bq[o][0][q], p);
-    if (r > 8) {
+      for (int q = 1; q < WAVES; q++) v += red[q][i][m][ln][u];
 #pragma unroll
-      for (int q = 0; q < 8; q++) p = fmaf(sp[tok][8 + q], (float)bq[o][1][q], p);
+      for (int q = 0; q < 8; q++) p = fmaf(sp[t][q], (float)bq[o][0][q], p);
+      if (r > 8) {
+#pragma unroll
+        for (int q = 0; q < 8; q++) p = fmaf(sp[t][8 + q], (float)bq[o][1][q], p);
+      }
+      a.y[(int64_t)t * w.n + n] = (bf16_t)fmaf(a.s, p, v);
     }
-    a.y[(int64_t)tok * w.n + n] = (bf16_t)fmaf(a.s, p, v);
   }
+}
+template <int NT, int MT> constexpr size_t few_lds() {
+  const size_t stage = (size_t)8 * MT * STAGE_BYTES, sums = (size_t)8 * (NT + 1) * MT * 1024 + (size_t)MT * 16 * 17 * 4;
+  return stage > sums ? stage : sums;
+}
+template <int NT, int MT, int PER, bool ONE>
+static hipError_t launch_few(const Q4Matrix &w, const Q4Few &a, hipStream_t st) {
+  constexpr size_t lds = few_lds<NT, MT>();
+  if constexpr (lds > 65536) {
+    static const hipError_t e = hipFuncSetAttribute((const void *)q4_few_kernel<NT, MT, PER, ONE>,
+                                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((q4_few_kernel<NT, MT, PER, ONE>), dim3((unsigned)((q4_row_blocks(w.n) + NT - 1) / NT)), dim3(512),
+                     lds, st, w, a);
+  return hipGetLastError();
+}
+template <int MT, int PER, bool ONE>
+static hipError_t launch_few_n(const Q4Matrix &w, const Q4Few &a, hipStream_t st) {
+  // as many tiles per workgroup as leave the chip one round of workgroups (4096 -> 11008 with one, two, three: 11.3,
+  // 9.4, 7.8 us; 4096 -> 4096 with one and three: 5.4, 6.8)
+  const int64_t tiles = q4_row_blocks(w.n);
+  if (tiles <= 256) return launch_few<1, MT, PER, ONE>(w, a, st);
+  if (tiles <= 512) return launch_few<2, MT, PER, ONE>(w, a, st);
+  return launch_few<3, MT, PER, ONE>(w, a, st);
+}
+template <int PER> static hipError_t launch_few_m(const Q4Matrix &w, const Q4Few &a, hipStream_t st) {
+  if (a.T == 1) return launch_few_n<1, PER, true>(w, a, st);
+  if (a.T <= 16) return launch_few_n<1, PER, false>(w, a, st);
+  if (a.T <= 32) return launch_few_n<2, PER, false>(w, a, st);
+  return launch_few_n<4, PER, false>(w, a, st);
 }
 
 // ---- everything else up to 128 rows: slices of the contraction, then their sum with the rank-r term --------
@@ -196,35 +295,48 @@ struct Q4Slices {
 template <int MT, int WM, int PER>
 __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4Slices z, DropArgs drop) {
   constexpr int NT = Q4S_NT, WK = 8 / WM;
-  extern __shared__ __align__(16) float red[];   // [8][NT][MT][64][4]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, hi = lane >> 4;
+  // wavefront by wavefront the staging of MT row blocks, then sums [8][NT][MT][64][4]
+  extern __shared__ __align__(16) unsigned char smem[];
+  float *red = reinterpret_cast<float *>(smem);
+  static_assert(NT >= 4, "the staging fits");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l15 = lane & 15, hi = lane >> 4;
   const int T = a.T, r = a.r, K = w.K, kbs = (int)q4_col_blocks(K);
   if ((int)blockIdx.x >= z.main) {   // a slice of the projection of 16 rows: one tile of the contraction per wavefront
     const int nq = (r + 15) >> 4, at = blockIdx.x - z.main, ps = at % z.PS, t0 = at / z.PS * 16;
     const int kb = ps * 8 + wave, row = t0 + l15 < T ? t0 + l15 : T - 1;
-    bf16x8_t fx[4];
+    unsigned char *stage = smem + wave * STAGE_BYTES;
+    f32x4_t p[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) p[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (kb < kbs) {
-      load_rows(a.x + (int64_t)row * K, kb * Q4_COLS, hi, K, fx);
+      bf16x8_t v[4], fx[4];
+      rows_load(a.x, RowOffsets(t0, T, K, lane), kb, K, lane, v);
+      rows_to_lds(stage, v, kb, K, lane);
+      wave_order();
+      rows_from_lds(stage, lane, fx);
       if (drop.thr) {
         const DropKey key = drop_key(drop);
 #pragma unroll
         for (int st = 0; st < 4; st++)
           fx[st] = drop_mask8(key, (uint32_t)row, (uint32_t)(kb * Q4_COLS + st * 32 + hi * 8) >> 3, fx[st]);
       }
-      zero_past(kb * Q4_COLS, hi, K, fx);
-    }
-    for (int j = 0; j < nq; j++) {
-      f32x4_t p = {0.f, 0.f, 0.f, 0.f};
-      if (kb < kbs) {
-        bf16x8_t fa[4];
-        const int q = j * 16 + l15;
-        load_rows(a.A + (int64_t)(q < r ? q : r - 1) * K, kb * Q4_COLS, hi, K, fa);
-        zero_past(kb * Q4_COLS, hi, K, fa);
 #pragma unroll
-        for (int st = 0; st < 4; st++) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[st], fa[st], p, 0, 0, 0);
+      for (int j = 0; j < 4; j++) {
+        if (j >= nq) break;
+        bf16x8_t fa[4];
+        rows_load(a.A, RowOffsets(j * 16, r, K, lane), kb, K, lane, v);
+        wave_order();
+        rows_to_lds(stage, v, kb, K, lane);
+        wave_order();
+        rows_from_lds(stage, lane, fa);
+#pragma unroll
+        for (int st = 0; st < 4; st++) p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[st], fa[st], p[j], 0, 0, 0);
       }
-      *reinterpret_cast<f32x4_t *>(red + ((wave * 4 + j) * 64 + lane) * 4) = p;
     }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      if (j < nq) *reinterpret_cast<f32x4_t *>(red + ((wave * 4 + j) * 64 + lane) * 4) = p[j];
     __syncthreads();
     for (int i = tid; i < nq * 256; i += 512) {
       const int j = i >> 8, q = j * 16 + (i & 15), tl = (i >> 4) & 15;
@@ -241,43 +353,47 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
   const int row_blocks = (int)q4_row_blocks(w.n);
   const int wm = wave / WK, wk = wave % WK;
   const int lo = sl * z.per, end = lo + z.per < kbs ? lo + z.per : kbs;
-  const bf16_t *xr[MT];
+  int64_t first[NT];   // tiles in front of each row block
 #pragma unroll
-  for (int m = 0; m < MT; m++) {
-    const int t = (wm * MT + m) * 16 + l15;
-    xr[m] = a.x + (int64_t)(t < T ? t : T - 1) * K;
-  }
-  const unsigned char *cr[NT];
-  const bf16_t *sr[NT];
-#pragma unroll
-  for (int i = 0; i < NT; i++) {
-    const int64_t first = (int64_t)(rb0 + i < row_blocks ? rb0 + i : row_blocks - 1) * kbs;
-    cr[i] = w.codes + first * Q4_TILE_BYTES + 16 * lane;
-    sr[i] = w.scales + (first * Q4_ROWS + l15) * PER;
-  }
+  for (int i = 0; i < NT; i++) first[i] = (int64_t)(rb0 + i < row_blocks ? rb0 + i : row_blocks - 1) * kbs;
   f32x4_t acc[NT][MT];
 #pragma unroll
   for (int i = 0; i < NT; i++)
 #pragma unroll
     for (int m = 0; m < MT; m++) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int kb = lo + wk; kb < end; kb += WK) {
-    uint4 c[NT];
-    float s[NT][PER];
-    bf16x8_t fx[MT][4];
+  unsigned char *stage = smem + wave * MT * STAGE_BYTES;
+  uint4 nc[NT];
+  float ns[NT][PER];
+  auto load_w = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < NT; i++) {
-      c[i] = *reinterpret_cast<const uint4 *>(cr[i] + (int64_t)kb * Q4_TILE_BYTES);
-      q4_load_scales<PER>(sr[i] + (int64_t)kb * Q4_ROWS * PER, s[i]);
+      q4_load<PER>(w, first[i] + kb, lane, nc[i], ns[i]);
     }
+  };
+  if (lo + wk < end) load_w(lo + wk);
+  for (int kb = lo + wk; kb < end; kb += WK) {
+    bf16x8_t fx[MT][4], x[MT][4];
 #pragma unroll
-    for (int m = 0; m < MT; m++) load_rows(xr[m], kb * Q4_COLS, hi, K, fx[m]);
-    if (kb == kbs - 1) {
+    for (int m = 0; m < MT; m++) rows_load(a.x, RowOffsets((wm * MT + m) * 16, T, K, lane), kb, K, lane, x[m]);
+    wave_order();
 #pragma unroll
-      for (int m = 0; m < MT; m++) zero_past(kb * Q4_COLS, hi, K, fx[m]);
+    for (int m = 0; m < MT; m++) rows_to_lds(stage + m * STAGE_BYTES, x[m], kb, K, lane);
+    uint4 c[NT];
+    float s[NT][PER];
+#pragma unroll
+    for (int i = 0; i < NT; i++) {
+      c[i] = nc[i];
+#pragma unroll
+      for (int g = 0; g < PER; g++) s[i][g] = ns[i][g];
     }
+    wave_order();
+    if (kb + WK < end) load_w(kb + WK);
+#pragma unroll
+    for (int m = 0; m < MT; m++) rows_from_lds(stage + m * STAGE_BYTES, lane, fx[m]);
 #pragma unroll
     for (int i = 0; i < NT; i++) q4_tile<MT, PER>(fx, c[i], s[i], acc[i]);
   }
+  __syncthreads();   // the staging is behind everybody
 #pragma unroll
   for (int i = 0; i < NT; i++)
 #pragma unroll
@@ -345,14 +461,18 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(int n, Q4Few a, Q4Slices
   *reinterpret_cast<bf16x4_t *>(a.y + (int64_t)t * n + c) = o;
 }
 
-static bool one_launch(int T, int r, bool drop) { return T <= 16 && r <= 16 && !drop; }
+// Where the one launch is the shorter way (us, one launch / slices and their sum): 17 tokens 4096 -> 1024 7.1 / 9.3, 24
+// tokens 5120 -> 5120 10.3 / 13.3, 64 tokens 4096 -> 4096 14.7 / 17.3; 32 tokens 11008 -> 4096 17.4 / 18.7, but 64
+// of them 30.4 / 23.9: four row blocks of x over a long contraction.
+static bool one_launch(int T, int K, int r, bool drop) { return T <= (K <= 8192 ? 64 : 32) && r <= 16 && !drop; }
 
-// Slices of the contraction: enough workgroups for the chip twice, no wavefront without a tile.
-static Q4Slices plan_slices(int n, int K, int T, int r) {
+// Slices of the contraction: as many workgroups as fit the chip in one round (128 tokens 4096 -> 4096 with two rounds of
+// them 28.4 us, with one 21.1; 48 tokens 4096 -> 11008 34.5, 24.0), no wavefront without a tile.
+static Q4Slices plan_slices(int n, int K, int T) {
   Q4Slices z{};
   const int kbs = (int)q4_col_blocks(K), groups = (int)((q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT);
   const int wk = T <= 64 ? 8 : 4;
-  int S = (512 + groups - 1) / groups;
+  int S = 256 / groups;
   const int most = (kbs + wk - 1) / wk;
   S = S > most ? most : S < 1 ? 1 : S > 16 ? 16 : S;
   z.per = (kbs + S - 1) / S;
@@ -363,32 +483,25 @@ static Q4Slices plan_slices(int n, int K, int T, int r) {
 }
 
 size_t q4_few_scratch_floats(int n, int K, int T, int r) {
-  if (T > Q4_FEW_ROWS) return 0;
-  const Q4Slices z = plan_slices(n, K, T, r);   // (dropout, which one launch does not take, is not known yet)
+  if (T > Q4_FEW_ROWS || K >= 1 << 23) return 0;   // (32-bit offsets into x and A)
+  const Q4Slices z = plan_slices(n, K, T);   // (dropout, which one launch does not take, is not known yet)
   return (size_t)T * ((size_t)z.S * n + ((size_t)z.PS * r + 63) / 64 * 64) + 64;
 }
 
 hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop, float *scratch, size_t floats, hipStream_t st) {
-  if (a.T < 1 || a.T > Q4_FEW_ROWS || a.r % 8 || a.r > 64 || w.n % 8 || w.K % 8) return hipErrorInvalidValue;
+  if (a.T < 1 || a.T > Q4_FEW_ROWS || a.r % 8 || a.r > 64 || w.K >= 1 << 23 || w.n % 8 || w.K % 8) return hipErrorInvalidValue;
   const int slot = prof_on() ? prof_mark_begin(PROF_GEMM, st) : -1;
-  const int tiles = (int)q4_row_blocks(w.n);
 #define MIXLORA_BY_GROUP(LAUNCH)        \
   do {                                  \
     if (w.group == 128) LAUNCH(1);      \
     else if (w.group == 64) LAUNCH(2);  \
     else LAUNCH(4);                     \
   } while (0)
-  if (one_launch(a.T, a.r, drop.thr != 0)) {
-#define MIXLORA_FEW(NT_, PER_) \
-  hipLaunchKernelGGL((q4_few_kernel<NT_, PER_>), dim3((tiles + NT_ - 1) / NT_), dim3(512), 0, st, w, a)
-#define MIXLORA_FEW1(PER_) MIXLORA_FEW(1, PER_)
-#define MIXLORA_FEW2(PER_) MIXLORA_FEW(2, PER_)
-#define MIXLORA_FEW3(PER_) MIXLORA_FEW(3, PER_)
-    if (tiles <= 320) MIXLORA_BY_GROUP(MIXLORA_FEW1);
-    else if (tiles <= 512) MIXLORA_BY_GROUP(MIXLORA_FEW2);
-    else MIXLORA_BY_GROUP(MIXLORA_FEW3);
+  if (one_launch(a.T, w.K, a.r, drop.thr != 0)) {
+    const hipError_t e = w.group == 128 ? launch_few_m<1>(w, a, st) : w.group == 64 ? launch_few_m<2>(w, a, st) : launch_few_m<4>(w, a, st);
+    if (e != hipSuccess) return e;
   } else {
-    Q4Slices z = plan_slices(w.n, w.K, a.T, a.r);
+    Q4Slices z = plan_slices(w.n, w.K, a.T);
     if ((size_t)a.T * ((size_t)z.S * w.n + (size_t)z.PS * a.r) > floats) return hipErrorInvalidValue;
     z.part = scratch;
     z.ppart = scratch + (size_t)z.S * a.T * w.n;
