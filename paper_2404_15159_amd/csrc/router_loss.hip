@@ -5,17 +5,20 @@
 //   dz_ti = g_b a N / n p_ti (F_i - sum_j F_j p_tj) + g_z b 2 / n lse_t p_ti + [i kept] w_ti (dw_ti - sum_j w_tj dw_tj).
 // A token that the mask drops is left out of every sum, whatever its logits are, and gets index -1, weight 0
 // and a zero gradient.  Both directions read the logits once and are bound by a launch's latency (1 MB of
-// logits at 16384 x 16), so a thread takes a token and keeps its row in registers.  No sum depends on the
-// order in which workgroups end: their partial sums are added in a fixed order.
+// logits at 16384 x 16), so a thread takes a token and keeps its row in registers.  Sums over tokens are made on the
+// vector ALU, counts from ballots.  No sum depends on the order in which workgroups end: their partial sums are added
+// in a fixed order, by a launch of its own.
 #include "common.h"
 
 #include <cmath>
+#include <type_traits>
 
 using namespace mixlora;
 
 namespace {
 
-constexpr int RL_THREADS = 256;
+constexpr int RL_THREADS = 64;   // one wavefront: 16384 tokens are one workgroup per CU
+constexpr int RL_ALL = 1024;     // tokens that one workgroup takes, where a row fits the registers that leaves (N <= 16)
 struct RouterArgs {
   const void *logits;
   const unsigned char *mask;
@@ -23,16 +26,27 @@ struct RouterArgs {
   float balance, zc;
   int32_t *idx;
   float *w;
-  float *part;          // [workgroup][2 N + 2]: P sums, counts (all k, as whole numbers), z sum, tokens; counts of slot 0 behind
+  float *part;          // [wavefront][3 N + 2]: P sums, counts of all slots, of slot 0 (whole numbers), z sum, tokens
   float *stats;         // [N + 1]: F, then 1 / n (0 where no token is kept)
   float *loss;
   int32_t *counts;
 };
 
-template <typename E, int NR>
+// A row in registers, -inf past N.  FULL: N == NR, whole 16-byte pieces.
+template <typename E, int NR, bool FULL>
 __device__ __forceinline__ void load_row(const E *row, int N, float (&z)[NR]) {
+  if constexpr (FULL) {
 #pragma unroll
-  for (int i = 0; i < NR; i++) z[i] = i < N ? to_f32(row[i]) : -INFINITY;
+    for (int i = 0; i < NR; i += 8) {
+      Vec8<E> v;
+      v.load(row + i);
+#pragma unroll
+      for (int e = 0; e < 8; e++) z[i + e] = v.get(e);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NR; i++) z[i] = i < N ? to_f32(row[i]) : -INFINITY;
+  }
 }
 
 // softmax of a row in registers: z becomes p; returns lse.  A row of -inf alone gives NaN, as its definition does.
@@ -53,91 +67,46 @@ __device__ __forceinline__ float softmax_row(float (&z)[NR], int N) {
   return top + logf(sum);
 }
 
-template <typename E, int NR>
-__global__ __launch_bounds__(RL_THREADS) void router_loss_forward_kernel(RouterArgs a) {
-  __shared__ float col[RL_THREADS / 64][NR];
-  __shared__ int cnt[NR], first[NR];
-  __shared__ float zs[RL_THREADS / 64];
-  __shared__ int toks;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = a.N, k = a.k;
-  for (int i = tid; i < NR; i += RL_THREADS) cnt[i] = first[i] = 0;
-  if (tid == 0) toks = 0;
-  __syncthreads();
-  const int64_t t = (int64_t)blockIdx.x * RL_THREADS + tid;
-  const bool on = t < a.T && (!a.mask || a.mask[t]);
-  float z[NR], lse = 0.f;
-  if (on) {
-    load_row<E, NR>((const E *)a.logits + t * N, N, z);
-    // the k largest; NaN ranks with -inf
-    uint64_t taken = 0;
-    float raw[NR];
-#pragma unroll
-    for (int i = 0; i < NR; i++) raw[i] = isnan(z[i]) ? -INFINITY : z[i];
-    lse = softmax_row<NR>(z, N);
-    float sum = 0.f;
-    int32_t *idx = a.idx + t * k;
-    float *w = a.w + t * k;
-    for (int j = 0; j < k; j++) {
-      int best = -1;
-      float bz = 0.f, bp = 0.f;
-#pragma unroll
-      for (int i = 0; i < NR; i++) {
-        if (i < N && !(taken >> i & 1)) {
-          if (best < 0 || raw[i] > bz) best = i, bz = raw[i], bp = z[i];
-        }
-      }
-      taken |= 1ull << best;
-      idx[j] = best;
-      w[j] = bp;
-      sum += bp;
-      atomicAdd(&cnt[best], 1);          // whole numbers: any order gives the same
-      if (j == 0) atomicAdd(&first[best], 1);
-    }
-    for (int j = 0; j < k; j++) w[j] /= sum;
-    atomicAdd(&toks, 1);
-  } else {
-#pragma unroll
-    for (int i = 0; i < NR; i++) z[i] = 0.f;
-    if (t < a.T)
-      for (int j = 0; j < k; j++) a.idx[t * k + j] = -1, a.w[t * k + j] = 0.f;
-  }
-#pragma unroll
-  for (int i = 0; i < NR; i++) {
-    float v = z[i];
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-    if (lane == 0) col[wave][i] = v;
-  }
-  float v = lse * lse;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-  if (lane == 0) zs[wave] = v;
-  __syncthreads();
-  float *p = a.part + (int64_t)blockIdx.x * (3 * N + 2);
-  for (int i = tid; i < N; i += RL_THREADS) {
-    float s = 0.f;
-    for (int u = 0; u < RL_THREADS / 64; u++) s += col[u][i];
-    p[i] = s;
-    p[N + i] = (float)cnt[i];            // at most 256 k: exact
-    p[2 * N + i] = (float)first[i];
-  }
-  if (tid == 0) {
-    float s = 0.f;
-    for (int u = 0; u < RL_THREADS / 64; u++) s += zs[u];
-    p[3 * N] = s;
-    p[3 * N + 1] = (float)toks;
-  }
+// sum over the wavefront on the vector ALU (lanes exchange with their quad, half row, row, then rows), for all lanes
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_total(float v) {
+  v = dpp_add<0xb1>(v);    // quad_perm 1 0 3 2
+  v = dpp_add<0x4e>(v);    // quad_perm 2 3 0 1
+  v = dpp_add<0x141>(v);   // row_half_mirror
+  v = dpp_add<0x140>(v);   // row_mirror: every lane has its row's sum
+  const int b = __builtin_bit_cast(int, v);
+  auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(b, l)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
 }
 
-// Adds the workgroups' sums, in double and in their order.
-__global__ __launch_bounds__(256) void router_loss_finish_kernel(RouterArgs a, int blocks) {
+// Adds the wavefronts' sums in double, each thread every G-th of them, then the G sums in order; called by all of a
+// workgroup of `threads`, at least 3 N + 2.
+__device__ void finish(const RouterArgs &a, int blocks, int threads) {
+  __shared__ double part[1024];
   __shared__ double sums[3 * 64 + 2];
   __shared__ double fp[64];
-  const int W = 3 * a.N + 2, tid = threadIdx.x;
-  for (int i = tid; i < W; i += 256) {
+  const int W = 3 * a.N + 2, tid = threadIdx.x, G = threads / W;
+  const int i = tid % W, g = tid / W;
+  if (g < G) {
     double s = 0.0;
-    for (int b = 0; b < blocks; b++) s += a.part[(int64_t)b * W + i];
-    sums[i] = s;
+    constexpr int INFLIGHT = 8;
+    for (int b = g; b < blocks; b += INFLIGHT * G) {
+      float v[INFLIGHT];
+#pragma unroll
+      for (int u = 0; u < INFLIGHT; u++) v[u] = a.part[(int64_t)(b + u * G < blocks ? b + u * G : b) * W + i];
+#pragma unroll
+      for (int u = 0; u < INFLIGHT; u++)
+        if (b + u * G < blocks) s += v[u];
+    }
+    part[tid] = s;
+  }
+  __syncthreads();
+  if (tid < W) {
+    double s = 0.0;
+    for (int u = 0; u < G; u++) s += part[u * W + tid];
+    sums[tid] = s;
   }
   __syncthreads();
   const double n = sums[3 * a.N + 1], inv = n > 0 ? 1.0 / n : 0.0;
@@ -150,7 +119,7 @@ __global__ __launch_bounds__(256) void router_loss_finish_kernel(RouterArgs a, i
   __syncthreads();
   if (tid == 0) {
     double s = 0.0;
-    for (int i = 0; i < a.N; i++) s += fp[i];
+    for (int e = 0; e < a.N; e++) s += fp[e];
     const double balance = (double)a.balance * a.N * s, z = (double)a.zc * sums[3 * a.N] * inv;
     a.loss[0] = (float)(balance + z);
     a.loss[1] = (float)balance;
@@ -159,58 +128,145 @@ __global__ __launch_bounds__(256) void router_loss_finish_kernel(RouterArgs a, i
   }
 }
 
-template <typename E, int NR>
+// ALL: one workgroup takes every token and adds its wavefronts' sums itself.
+template <typename E, int NR, bool FULL, bool ALL>
+__global__ __launch_bounds__(ALL ? RL_ALL : RL_THREADS) void router_loss_forward_kernel(RouterArgs a) {
+  const int lane = threadIdx.x & 63, N = FULL ? NR : a.N, k = a.k;
+  const int wave = blockIdx.x + (threadIdx.x >> 6);
+  const int64_t t = (int64_t)wave * RL_THREADS + lane;
+  const bool on = t < a.T && (!a.mask || a.mask[t]);
+  float z[NR], lse = 0.f;
+  uint64_t taken = 0;
+  int first = -1;
+  if (on) {
+    load_row<E, NR, FULL>((const E *)a.logits + t * N, N, z);
+    float raw[NR];   // NaN ranks with -inf
+#pragma unroll
+    for (int i = 0; i < NR; i++) raw[i] = isnan(z[i]) ? -INFINITY : z[i];
+    lse = softmax_row<NR>(z, N);
+    constexpr int KEEP = 8;   // weights that wait in registers for their sum; further ones wait in memory
+    float sum = 0.f, wk[KEEP];
+    int32_t *idx = a.idx + t * k;
+    float *w = a.w + t * k;
+    auto pick = [&](int &best, float &bp) {   // the largest that is left, the lowest index among equals
+      best = -1;
+      float bz = 0.f;
+#pragma unroll
+      for (int i = 0; i < NR; i++) {
+        if (i < N && !(taken >> i & 1) && (best < 0 || raw[i] > bz)) best = i, bz = raw[i], bp = z[i];
+      }
+      taken |= 1ull << best;
+      sum += bp;
+    };
+#pragma unroll
+    for (int j = 0; j < KEEP; j++) {
+      if (j >= k) break;
+      int best;
+      pick(best, wk[j]);
+      if (j == 0) first = best;
+      idx[j] = best;
+    }
+    for (int j = KEEP; j < k; j++) {
+      int best;
+      float bp = 0.f;
+      pick(best, bp);
+      idx[j] = best;
+      w[j] = bp;
+    }
+#pragma unroll
+    for (int j = 0; j < KEEP; j++)
+      if (j < k) w[j] = wk[j] / sum;
+    for (int j = KEEP; j < k; j++) w[j] /= sum;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NR; i++) z[i] = 0.f;
+    if (t < a.T)
+      for (int j = 0; j < k; j++) a.idx[t * k + j] = -1, a.w[t * k + j] = 0.f;
+  }
+  // lane i keeps expert i's sums
+  float P = 0.f, all = 0.f, slot0 = 0.f;
+#pragma unroll
+  for (int i = 0; i < NR; i++) {
+    if (i < N) {   // (uniform)
+      const float s = wave_total(z[i]);
+      const int c = __popcll(__ballot(taken >> i & 1)), f = __popcll(__ballot(first == i));
+      if (lane == i) P = s, all = (float)c, slot0 = (float)f;
+    }
+  }
+  const float zs = wave_total(lse * lse);
+  const float n = (float)__popcll(__ballot(on));
+  float *p = a.part + (int64_t)wave * (3 * N + 2);
+  if (lane < N) p[lane] = P, p[N + lane] = all, p[2 * N + lane] = slot0;
+  if (lane == 0) p[3 * N] = zs, p[3 * N + 1] = n;
+  if constexpr (ALL) {
+    __threadfence_block();
+    __syncthreads();
+    finish(a, blockDim.x >> 6, blockDim.x);
+  }
+}
+
+__global__ __launch_bounds__(1024) void router_loss_finish_kernel(RouterArgs a, int waves) { finish(a, waves, 1024); }
+
+template <typename E, int NR, bool FULL>
 __global__ __launch_bounds__(RL_THREADS) void router_loss_backward_kernel(RouterArgs a, const int32_t *__restrict__ idx,
                                                                           const float *__restrict__ dw, float gb, float gz,
                                                                           void *__restrict__ dz) {
   const int64_t t = (int64_t)blockIdx.x * RL_THREADS + threadIdx.x;
   if (t >= a.T) return;
-  const int N = a.N, k = a.k;
-  E *out = (E *)dz + t * N;
+  const int N = FULL ? NR : a.N, k = a.k;
+  float g[NR];
   if (a.mask && !a.mask[t]) {
-    for (int i = 0; i < N; i++) out[i] = from_f32<E>(0.f);
-    return;
-  }
-  float z[NR];
-  load_row<E, NR>((const E *)a.logits + t * N, N, z);
-  const float lse = softmax_row<NR>(z, N);
-  const float inv = a.stats[N];
-  float fp = 0.f;
 #pragma unroll
-  for (int i = 0; i < NR; i++)
-    if (i < N) fp = fmaf(a.stats[i], z[i], fp);
-  const float cb = gb * a.balance * (float)N * inv, cz = gz * a.zc * 2.f * inv * lse;
-  // the kept experts' share: w = p / sum of the kept p
-  uint64_t kept = 0;
-  float sum = 0.f, dot = 0.f;
-  if (dw) {
-    for (int j = 0; j < k; j++) {
-      const int e = idx[t * k + j];
-      if (e >= 0 && e < N) kept |= 1ull << e;
+    for (int i = 0; i < NR; i++) g[i] = 0.f;
+  } else {
+    float z[NR];
+    load_row<E, NR, FULL>((const E *)a.logits + t * N, N, z);
+    // g: the gradient of a kept expert's weight
+#pragma unroll
+    for (int i = 0; i < NR; i++) g[i] = 0.f;
+    uint64_t kept = 0;
+    if (dw) {
+      for (int j = 0; j < k; j++) {
+        const int e = idx[t * k + j];
+        const float d = dw[t * k + j];
+        if (e >= 0 && e < N) kept |= 1ull << e;
+#pragma unroll
+        for (int i = 0; i < NR; i++) g[i] = i == e ? d : g[i];
+      }
     }
+    const float lse = softmax_row<NR>(z, N);
+    const float inv = a.stats[N];
+    float fp = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NR; i++) {
+      if (i < N) fp = fmaf(a.stats[i], z[i], fp);
+      sum += kept >> i & 1 ? z[i] : 0.f;
+    }
+    const float cb = gb * a.balance * (float)N * inv, cz = gz * a.zc * 2.f * inv * lse;
+    // w = p over the kept ones' sum;  dz = w (dw - sum_j w_j dw_j) + the losses' share
+    const float rs = kept ? 1.f / sum : 0.f;
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < NR; i++) dot = kept >> i & 1 ? fmaf(z[i] * rs, g[i], dot) : dot;
+#pragma unroll
+    for (int i = 0; i < NR; i++) {
+      const float l = i < N ? z[i] * (cb * (a.stats[i] - fp) + cz) : 0.f;
+      g[i] = kept >> i & 1 ? fmaf(z[i] * rs, g[i] - dot, l) : l;
+    }
+  }
+  E *out = (E *)dz + t * N;
+  if constexpr (FULL) {
+#pragma unroll
+    for (int i = 0; i < NR; i += 8) {
+      Vec8<E> v;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.set(e, g[i + e]);
+      v.store(out + i);
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < NR; i++)
-      if (i < N && (kept >> i & 1)) sum += z[i];
-    for (int j = 0; j < k; j++) {
-      const int e = idx[t * k + j];
-      float pe = 0.f;
-#pragma unroll
-      for (int i = 0; i < NR; i++)
-        if (i == e) pe = z[i];
-      dot = fmaf(pe / sum, dw[t * k + j], dot);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < NR; i++) {
-    if (i >= N) continue;
-    float g = z[i] * (cb * (a.stats[i] - fp) + cz);
-    if (kept >> i & 1) {
-      float d = 0.f;
-      for (int j = 0; j < k; j++)
-        if (idx[t * k + j] == i) d = dw[t * k + j];
-      g = fmaf(z[i] / sum, d - dot, g);
-    }
-    out[i] = from_f32<E>(g);
+      if (i < N) out[i] = from_f32<E>(g[i]);
   }
 }
 
@@ -235,20 +291,37 @@ RouterArgs args_of(const mixlora_router_dims &D, const void *logits, const unsig
   return a;
 }
 
-// one instance per storage type and row length
-#define MIXLORA_ROUTER(KERNEL, D, ...)                                                                                \
-  do {                                                                                                                \
-    const dim3 grid_(blocks_of((D).T)), block_(RL_THREADS);                                                           \
-    if ((D).dtype == MIXLORA_BF16) {                                                                                  \
-      if ((D).N <= 8) hipLaunchKernelGGL((KERNEL<bf16_t, 8>), grid_, block_, 0, st, __VA_ARGS__);                     \
-      else if ((D).N <= 16) hipLaunchKernelGGL((KERNEL<bf16_t, 16>), grid_, block_, 0, st, __VA_ARGS__);              \
-      else hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid_, block_, 0, st, __VA_ARGS__);                               \
-    } else {                                                                                                          \
-      if ((D).N <= 8) hipLaunchKernelGGL((KERNEL<float, 8>), grid_, block_, 0, st, __VA_ARGS__);                      \
-      else if ((D).N <= 16) hipLaunchKernelGGL((KERNEL<float, 16>), grid_, block_, 0, st, __VA_ARGS__);               \
-      else hipLaunchKernelGGL((KERNEL<float, 64>), grid_, block_, 0, st, __VA_ARGS__);                                \
-    }                                                                                                                 \
-  } while (0)
+template <typename E, int NR, bool FULL>
+hipError_t launch_forward(const RouterArgs &a, hipStream_t st) {
+  const int waves = blocks_of(a.T);
+  if constexpr (NR <= 16) {
+    if (a.T <= RL_ALL) {   // (300 x 8: 2.7 us of a second launch)
+      const int threads = waves * 64 < 64 ? 64 : waves * 64;
+      hipLaunchKernelGGL((router_loss_forward_kernel<E, NR, FULL, true>), dim3(1), dim3(threads), 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((router_loss_forward_kernel<E, NR, FULL, false>), dim3(waves), dim3(RL_THREADS), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(router_loss_finish_kernel, dim3(1), dim3(1024), 0, st, a, waves);
+  return hipGetLastError();
+}
+template <typename E, int NR, bool FULL>
+hipError_t launch_backward(const RouterArgs &a, const int32_t *idx, const float *dw, float gb, float gz, void *dz, hipStream_t st) {
+  hipLaunchKernelGGL((router_loss_backward_kernel<E, NR, FULL>), dim3(blocks_of(a.T)), dim3(RL_THREADS), 0, st, a, idx, dw, gb, gz, dz);
+  return hipGetLastError();
+}
+// one instance per storage type and row length, with whole rows of 8, 16 and 64 apart
+template <typename F>
+hipError_t by_row(int N, F &&f) {
+  if (N == 8) return f(std::integral_constant<int, 8>{}, std::true_type{});
+  if (N < 8) return f(std::integral_constant<int, 8>{}, std::false_type{});
+  if (N == 16) return f(std::integral_constant<int, 16>{}, std::true_type{});
+  if (N < 16) return f(std::integral_constant<int, 16>{}, std::false_type{});
+  if (N == 64) return f(std::integral_constant<int, 64>{}, std::true_type{});
+  return f(std::integral_constant<int, 64>{}, std::false_type{});
+}
 
 }  // namespace
 
@@ -272,10 +345,11 @@ int mixlora_router_loss_forward(const mixlora_router_dims *dims, const void *log
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   RouterArgs a = args_of(*dims, logits, token_mask, workspace);
   a.idx = topk_idx, a.w = topk_w, a.loss = loss, a.counts = counts;
-  MIXLORA_ROUTER(router_loss_forward_kernel, *dims, a);
-  if (hipGetLastError() != hipSuccess) return MIXLORA_E_HIP;
-  hipLaunchKernelGGL(router_loss_finish_kernel, dim3(1), dim3(256), 0, st, a, blocks_of(dims->T));
-  return hipGetLastError() == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
+  const hipError_t e = by_row(dims->N, [&](auto nr, auto full) {
+    return dims->dtype == MIXLORA_BF16 ? launch_forward<bf16_t, nr.value, full.value>(a, st)
+                                       : launch_forward<float, nr.value, full.value>(a, st);
+  });
+  return e == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
 }
 
 int mixlora_router_loss_backward(const mixlora_router_dims *dims, const void *logits, const unsigned char *token_mask,
@@ -289,8 +363,12 @@ int mixlora_router_loss_backward(const mixlora_router_dims *dims, const void *lo
   if (workspace_bytes < mixlora_router_loss_workspace_bytes(dims)) return MIXLORA_E_WORKSPACE;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const RouterArgs a = args_of(*dims, logits, token_mask, workspace);
-  MIXLORA_ROUTER(router_loss_backward_kernel, *dims, a, topk_idx, d_topk_w, d_balance, d_z, dlogits);
-  return hipGetLastError() == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
+  const hipError_t e = by_row(dims->N, [&](auto nr, auto full) {
+    return dims->dtype == MIXLORA_BF16
+               ? launch_backward<bf16_t, nr.value, full.value>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st)
+               : launch_backward<float, nr.value, full.value>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st);
+  });
+  return e == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
 }
 
 }  // extern "C"
