@@ -2,9 +2,8 @@
 //   y = x W^T + s (D(x) A^T) B^T,   dx = dy W + D'(s (dy B) A),   dA = s (dy B)^T D(x),   dB = s dy^T (D(x) A^T)
 // D drops elements and scales the others (dropout.h makes the mask from counters wherever it is needed),
 // D' drops the same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen
-// product as an extra K segment, in three bf16 pieces that hold all of its 24 bits, in the backward too
-// where there is no dropout; with dropout the product is made in fp32 and the masked term is added where it
-// is rounded, so that a result is rounded once.  The gradient sums take the rank-r factor in three pieces as
+// product as an extra K segment, in three bf16 pieces that hold all of its 24 bits; the backward's, which has to
+// be masked with dropout, goes first and is masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as
 // well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h), but for the forward of up to
 // 128 rows, which multiplies with the codes (q4_few.hip).
 #include "common.h"
@@ -68,7 +67,7 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   L.At = take(di * r * E);
   L.V = take(T * r * 4);
   L.V_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
-  L.dx32 = take(bf16 ? T * di * 4 : 0);
+  L.dx32 = take(bf16 && !gemm_masked_ok(D.T, D.d_in, D.d_out) ? T * di * 4 : 0);
   L.partial_floats = bf16 ? group_outer_mfma_partial_floats(1, (int)r, (int)di, (int)T, 2) +
                                 group_outer_mfma_partial_floats(1, (int)r, (int)dn, (int)T, 2)
                           : group_outer_partial_floats(1, (int)r, (int)di, (int)T) +
@@ -340,18 +339,28 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       const Project px{x, A, B, T, di, r, 0, L.ldT, s, P, ws + L.P_T, ws + L.ext, ws + L.ext_B, (int32_t *)(ws + L.offs)};
       HIP_TRY(launch_project(px, drop, st));
     }
-    const Project pr{dy, ws + L.Bt, ws + L.At, T, dn, r, di, L.ldT, s, V, ws + L.V_T, ws + L.ext, ws + L.ext_B,
-                     (int32_t *)(ws + L.offs)};
+    // (the term of dx is masked and scaled, the factor V of dA is not)
+    const Project pr{dy, ws + L.Bt, ws + L.At, T, dn, r, di, L.ldT, drop.thr ? s * drop.inv : s, V, ws + L.V_T, ws + L.ext,
+                     ws + L.ext_B, (int32_t *)(ws + L.offs)};
     HIP_TRY(launch_project(pr, DropArgs{}, st));
     const GemmScratch gs{L.gemm_floats ? (float *)(ws + L.gemm_part) : nullptr, L.gemm_floats};
-    GemmProblem p = problem(T, di, drop.thr ? (void *)(ws + L.dx32) : dx, drop.thr != 0, dy, W_T, dn);
+    const GemmSeg frozen{dy, W_T, dn, dn, dn}, term{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
+    GemmProblem p = problem(T, di, dx, 0, dy, W_T, dn);
     if (!drop.thr) {
-      p.seg[1] = GemmSeg{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
+      p.seg[1] = term;
       p.nseg = 2;
-    }
-    HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
-    if (drop.thr)
+      HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
+    } else if (gemm_masked_ok(T, di, dn)) {
+      p.seg[0] = term;
+      p.seg[1] = frozen;
+      p.nseg = 2;
+      HIP_TRY(launch_gemm_masked(p, drop, st, gs));
+    } else {   // operands of 4 GiB or more
+      p.C = ws + L.dx32;
+      p.c_f32 = 1;
+      HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
       HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
+    }
     const GomJob go[2] = {
         GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 3, drop},
         GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, 3, DropArgs{}}};

@@ -48,6 +48,15 @@ template <> struct Vec8<float> {
   }
 };
 
+// Dropout of a matrix's elements (csrc/dropout.h has the generator)
+struct DropArgs {
+  uint32_t thr;             // an element is dropped where its 16 bits are below thr; 0: nothing is dropped
+  float inv;                // 65536 / (65536 - thr), the factor of the others
+  uint32_t k0, k1;          // the seed
+  uint64_t offset;
+  const uint64_t *step;     // device, may be NULL: added to offset when a kernel runs
+};
+
 // ---- GEMM engine:  C[M,N] = sum over segments  A_s[M,K_s] * B_s[N,K_s]^T -----------------
 // Both operands are K-contiguous ("NT").  K_s % 8 == 0, lda/ldb % 8 == 0, 16-byte aligned
 // bases.  C is written in the storage dtype or as float32.
@@ -81,6 +90,10 @@ struct GemmScratch {
 // that its sums are taken in the same order.
 hipError_t launch_gemm(int dtype, const GemmProblem *probs, int nprob, hipStream_t st,
                        const GemmScratch &scratch = GemmScratch{nullptr, 0}, int only = -1);
+// bf16: the first segment's product (K <= 192, say) counts only where drop keeps an element of C (row and column of C),
+// unscaled; the others are added to it.  On the large tiles whatever M; operands below 4 GiB (gemm_masked_ok).
+bool gemm_masked_ok(int M, int N, int K);
+hipError_t launch_gemm_masked(const GemmProblem &p, const DropArgs &drop, hipStream_t st, const GemmScratch &scratch);
 // the row kernel with the rank-r term of the down projection added, for one or two tokens
 struct FewRank;
 // the few-rows kernel over K slices of the down projection, and the rank term's sums in further workgroups
@@ -397,15 +410,6 @@ constexpr int GO_MAX_JOBS = 7;
 hipError_t launch_group_outer(const GoJob *jobs, int njobs, float *partials, size_t partial_floats,
                               hipStream_t st);
 size_t group_outer_partial_floats(int G, int r, int C, int rows);
-
-// Dropout of a matrix's elements (csrc/dropout.h has the generator)
-struct DropArgs {
-  uint32_t thr;             // an element is dropped where its 16 bits are below thr; 0: nothing is dropped
-  float inv;                // 65536 / (65536 - thr), the factor of the others
-  uint32_t k0, k1;          // the seed
-  uint64_t offset;
-  const uint64_t *step;     // device, may be NULL: added to offset when a kernel runs
-};
 
 // bf16 MFMA version: smallT is the transposed bf16 factor [r][ldT] (ldT % 8 == 0, readable up to
 // the next multiple of 16 rows past the last group), wide is bf16 with C % 8 == 0.  Up to

@@ -288,7 +288,7 @@ constexpr int Q4S_NT = 4;
 struct Q4Slices {
   int S, per;              // slices, tiles of each
   int main;                // workgroups of the product
-  int PS, pper;            // slices of the projection, in tiles (at most 8: one per wavefront)
+  int PS;                  // slices of the projection, of eight tiles: one per wavefront
   float *part, *ppart;     // [S][T][n], [PS][T][r]
 };
 
