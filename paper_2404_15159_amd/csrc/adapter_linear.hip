@@ -9,7 +9,8 @@
 #include "common.h"
 #include "q4.h"
 #include "q4_few.h"
-#include "rank_project.h"
+#include "dropout.h"
+#include "rows_stage.h"
 
 #include <cmath>
 #include <initializer_list>
@@ -25,12 +26,14 @@ inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) &
 struct Layout {
   int rp, ldT;                            // rank rounded up to a multiple of 8; pitch of the transposed factors
   size_t padA, padB, P, P_T, offs;        // kept for the backward
-  size_t ext, ext_B, gemm_part, xd;       // scratch of either direction
+  size_t ext, ext_B, proj, gemm_part, xd; // scratch of either direction
   size_t W, fwd_end;
   size_t W_T, Bt, At, V, V_T, dx32, partials, padgA, padgB, bwd_end;
   size_t few;                             // partial sums of the few-rows product
   size_t gemm_floats, partial_floats, few_floats;
 };
+
+size_t project_floats(int T, int K, int r);   // partial sums of a projection
 
 // q4: room for the widened matrix.  The scratch of the two directions overlaps.
 Layout make_layout(const mixlora_linear_dims &D, bool q4) {
@@ -49,6 +52,10 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   L.offs = take(2 * 4);
   L.ext = take(bf16 ? T * 3 * r * 2 : 0);
   L.ext_B = take(bf16 ? wide * 3 * r * 2 : 0);
+  {
+    const size_t fx = project_floats(D.T, D.d_in, (int)r), fdy = project_floats(D.T, D.d_out, (int)r);
+    L.proj = take(bf16 ? (fx > fdy ? fx : fdy) * 4 : 0);
+  }
   {   // partial tiles of products cut along K: at most one tile per CU
     const size_t slices = wide / 64 / 4, tiles = (T / 192 + 1) * (wide / 256 + 1) * slices;
     L.gemm_floats = bf16 && slices >= 2 ? GEMM_SCRATCH_FLOATS / 256 * (tiles < 256 ? tiles : 256) : 0;
@@ -68,8 +75,7 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   L.V = take(T * r * 4);
   L.V_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
   L.dx32 = take(bf16 && !gemm_masked_ok(D.T, D.d_in, D.d_out) ? T * di * 4 : 0);
-  L.partial_floats = bf16 ? group_outer_mfma_partial_floats(1, (int)r, (int)di, (int)T, 2) +
-                                group_outer_mfma_partial_floats(1, (int)r, (int)dn, (int)T, 2)
+  L.partial_floats = bf16 ? adapter_sums_partial_floats((int)r, (int)di, (int)T) + adapter_sums_partial_floats((int)r, (int)dn, (int)T)
                           : group_outer_partial_floats(1, (int)r, (int)di, (int)T) +
                                 group_outer_partial_floats(1, (int)r, (int)dn, (int)T);
   L.partials = take(L.partial_floats * 4);
@@ -83,7 +89,7 @@ int check_dims(const mixlora_linear_dims *D) {
   if (!D) return MIXLORA_E_NULL;
   if (D->dtype != MIXLORA_F32 && D->dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
   if (D->T < 1 || D->d_in < 8 || D->d_out < 8 || D->r < 1 || D->r > 64) return MIXLORA_E_SHAPE;
-  if (D->d_in % 8 || D->d_out % 8) return MIXLORA_E_SHAPE;
+  if (D->d_in % 8 || D->d_out % 8 || D->d_in >= 1 << 27 || D->d_out >= 1 << 27) return MIXLORA_E_SHAPE;
   if ((int64_t)D->T >= (1 << 24)) return MIXLORA_E_SHAPE;
   return MIXLORA_OK;
 }
@@ -198,36 +204,185 @@ GemmProblem problem(int M, int N, void *C, int c_f32, const void *A, const void 
   return p;
 }
 
-// bf16: the projection P = D(X) Wq^T [T, r] in all its forms, and the other factor of the rank-r term for
-// cols columns from Wr [cols, r]
+// ---- bf16: the projection P = D(X) Wq^T [T, r] in all its forms ------------------------------------------------
+// P in fp32; PT, the row factor of the gradient sums, in three bf16 pieces [hi(r) | mid(r) | lo(r)][ldT]; and m P
+// (s = m 2^e, 1/2 <= |m| < 1) in three pieces, ext[t] = [hi(r) | mid(r) | lo(r)], whose sum is m P to its last bit.
+// The other factor of the rank-r term, from Wr [cols, r], is ext_B[c] = [B | B' | B'] 2^e with B' = B but zeros for
+// infinities: hi alone meets those, or two pieces of opposite signs would make NaN of them.
 struct Project {
-  const void *X, *Wq, *Wr;
-  int T, K, r, cols, ldT;
-  float s, *P;
-  void *PT, *ext, *ext_B;
+  const bf16_t *X, *Wq, *Wr;
+  int T, K, r, cols, ldT, S;   // S slices of the contraction, of `per` tiles
+  int per;
+  float m, b_scale, *P, *part; // part [S][T][r], S > 1
+  bf16_t *PT, *ext, *ext_B;
   int32_t *offs;
+  DropArgs drop;
 };
-hipError_t launch_project(const Project &a, const DropArgs &drop, hipStream_t st) {
+
+// v as the sum of three bf16 values, cut off by truncation; infinities and NaN stay in the first
+__device__ __forceinline__ void three_pieces(float v, float (&pc)[3]) {
+  const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
+  pc[0] = finite ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
+  const float rest = finite ? v - pc[0] : 0.f;
+  pc[1] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+  pc[2] = rest - pc[1];
+}
+__device__ __forceinline__ void store_projection(const Project &a, int t, int q, float v) {
+  if (a.drop.thr) v *= a.drop.inv;
+  a.P[(int64_t)t * a.r + q] = v;
+  float pc[3];
+  three_pieces(v, pc);
+#pragma unroll
+  for (int i = 0; i < 3; i++) a.PT[((int64_t)i * a.r + q) * a.ldT + t] = (bf16_t)pc[i];
+  three_pieces(a.m * v, pc);
+  bf16_t *o = a.ext + (int64_t)t * 3 * a.r + q;
+#pragma unroll
+  for (int i = 0; i < 3; i++) o[i * a.r] = (bf16_t)pc[i];
+}
+
+// Bound by reading X once.  A workgroup owns 16 rows and a slice of the contraction, its wavefronts 128-column tiles
+// of that in turn; both operands change lanes in LDS (rows_stage.h).  Few rows are cut into slices that fill the chip, which
+// project_finish_kernel adds in order; trailing workgroups lay out the other factor.
+template <int NQ, bool DROP, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void project_kernel(Project a) {
+  __shared__ __align__(16) unsigned char smem[WAVES * STAGE_BYTES];   // then sums [WAVES][NQ][64][4]
+  static_assert(NQ * 1024 <= STAGE_BYTES, "the sums fit");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = a.T, K = a.K, r = a.r, row_blocks = (T + 15) >> 4;
+  if ((int)blockIdx.x >= row_blocks * a.S) {   // workgroup-uniform; eight entries of a row of Wr per thread
+    const int per = r >> 3;
+    const int64_t i = (int64_t)(blockIdx.x - row_blocks * a.S) * (WAVES * 64) + tid;
+    if (i >= (int64_t)a.cols * per) return;
+    const int c = (int)(i / per), q0 = (int)(i % per) * 8;
+    bf16x8_t v = *reinterpret_cast<const bf16x8_t *>(a.Wr + (int64_t)c * r + q0), fin;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      v[e] = (bf16_t)((float)v[e] * a.b_scale);
+      fin[e] = __builtin_isinf((float)v[e]) ? (bf16_t)0.f : v[e];
+    }
+    bf16_t *o = a.ext_B + (int64_t)c * 3 * r + q0;
+    *reinterpret_cast<bf16x8_t *>(o) = v;
+    *reinterpret_cast<bf16x8_t *>(o + r) = fin;
+    *reinterpret_cast<bf16x8_t *>(o + 2 * r) = fin;
+    return;
+  }
+  if (blockIdx.x == 0 && tid == 0) {   // all tokens are one group of the gradient sums
+    a.offs[0] = 0;
+    a.offs[1] = T;
+  }
+  const int t0 = blockIdx.x % row_blocks * 16, sl = blockIdx.x / row_blocks;
+  const int kbs = (K + STAGE_COLS - 1) / STAGE_COLS, lo = sl * a.per, end = lo + a.per < kbs ? lo + a.per : kbs;
+  unsigned char *stage = smem + wave * STAGE_BYTES;
+  DropKey key;
+  if constexpr (DROP) key = drop_key(a.drop);
+  f32x4_t acc[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; j++) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int kb = lo + wave; kb < end; kb += WAVES) {
+    bf16x8_t vx[4], vw[NQ][4], fx[4];
+    rows_load(a.X + (int64_t)t0 * K, T - t0, kb, K, lane, vx);
+#pragma unroll
+    for (int j = 0; j < NQ; j++) rows_load(a.Wq + (int64_t)(j * 16 < r ? j * 16 : 0) * K, j * 16 < r ? r - j * 16 : r, kb, K, lane, vw[j]);
+    if constexpr (DROP) {   // a load is eight columns of a row: one call of the generator
+#pragma unroll
+      for (int p = 0; p < 4; p++)
+        vx[p] = drop_mask8(key, (uint32_t)(t0 + p * 4 + (lane >> 4)), (uint32_t)(kb * (STAGE_COLS / 8) + (lane & 15)), vx[p]);
+    }
+    wave_order();
+    rows_to_lds(stage, vx, kb, K, lane);
+    wave_order();
+    rows_from_lds(stage, lane, fx);
+#pragma unroll
+    for (int j = 0; j < NQ; j++) {
+      bf16x8_t fw[4];
+      wave_order();
+      rows_to_lds(stage, vw[j], kb, K, lane);
+      wave_order();
+      rows_from_lds(stage, lane, fw);
+#pragma unroll
+      for (int st = 0; st < 4; st++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[st], fx[st], acc[j], 0, 0, 0);
+    }
+  }
+  __syncthreads();   // the staging is behind everybody
+  float *red = reinterpret_cast<float *>(smem);
+#pragma unroll
+  for (int j = 0; j < NQ; j++) *reinterpret_cast<f32x4_t *>(red + ((wave * NQ + j) * 64 + lane) * 4) = acc[j];
+  __syncthreads();
+  // acc[j][u] of lane (l15, hi): row l15, q = 16 j + 4 hi + u
+  for (int i = tid; i < NQ * 256; i += WAVES * 64) {
+    const int j = i >> 8, q = j * 16 + (i & 15), t = t0 + ((i >> 4) & 15);
+    if (q >= r || t >= T) continue;
+    const int e = (((i >> 2) & 3) * 16 + ((i >> 4) & 15)) * 4 + (i & 3);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) v += red[(w * NQ + j) * 256 + e];
+    if (a.S == 1) store_projection(a, t, q, v);
+    else a.part[((int64_t)sl * T + t) * r + q] = v;
+  }
+}
+__global__ __launch_bounds__(256) void project_finish_kernel(Project a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.T * a.r;
+  if (i >= n) return;
+  float v = 0.f;
+  for (int s0 = 0; s0 < a.S; s0 += 8) {
+    float u[8];
+#pragma unroll
+    for (int s = 0; s < 8; s++) u[s] = a.part[(int64_t)(s0 + s < a.S ? s0 + s : s0) * n + i];
+#pragma unroll
+    for (int s = 0; s < 8; s++)
+      if (s0 + s < a.S) v += u[s];
+  }
+  store_projection(a, (int)(i / a.r), (int)(i % a.r), v);
+}
+
+// Slices of the projection: none where the row blocks alone nearly fill the chip, else as many as fill it with eight
+// tiles or fewer left to each.
+int project_slices(int T, int K) {
+  const int rb = (T + 15) / 16, kbs = (K + STAGE_COLS - 1) / STAGE_COLS;
+  if (rb >= 160) return 1;
+  const int want = 256 / rb, most = (kbs + 7) / 8;
+  return want < most ? want : most;
+}
+size_t project_floats(int T, int K, int r) {
+  const int S = project_slices(T, K);
+  return S > 1 ? (size_t)S * T * r : 0;
+}
+hipError_t launch_project(Project a, float s, const DropArgs &drop, hipStream_t st) {
   int e = 0;   // s = m 2^e
-  if (std::isfinite(a.s)) std::frexp(a.s, &e);
+  if (std::isfinite(s)) std::frexp(s, &e);
   e = e < -100 ? -100 : e > 100 ? 100 : e;
-  const float m = std::ldexp(a.s, -e);
-  const dim3 grid((a.T + 15) / 16 + ((int64_t)a.cols * (a.r / 8) + 511) / 512), block(512);
+  a.m = std::ldexp(s, -e);
+  a.b_scale = std::ldexp(1.f, e);
+  a.drop = drop;
+  const int kbs = (a.K + STAGE_COLS - 1) / STAGE_COLS;
+  a.S = project_slices(a.T, a.K);
+  a.per = (kbs + a.S - 1) / a.S;
+  a.S = (kbs + a.per - 1) / a.per;
   const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
-#define MIXLORA_PROJECT(NQ_, DROP_)                                                                          \
-  hipLaunchKernelGGL((rank_project_kernel<NQ_, DROP_, true>), grid, block, 0, st, (const bf16_t *)a.X,       \
-                     (const bf16_t *)a.Wq, a.T, a.K, a.r, m, a.P, (bf16_t *)a.PT, a.ldT, (bf16_t *)a.ext,    \
-                     a.offs, (const bf16_t *)a.Wr, a.cols, std::ldexp(1.f, e), (bf16_t *)a.ext_B, drop)
+#define MIXLORA_PROJECT(NQ_, DROP_, WAVES_)                                                                            \
+  hipLaunchKernelGGL((project_kernel<NQ_, DROP_, WAVES_>),                                                             \
+                     dim3((a.T + 15) / 16 * a.S + ((int64_t)a.cols * (a.r / 8) + WAVES_ * 64 - 1) / (WAVES_ * 64)),    \
+                     dim3(WAVES_ * 64), 0, st, a)
+#define MIXLORA_PROJECT_W(NQ_, DROP_)                   \
+  do {                                                  \
+    if (a.S > 1 || NQ_ > 2) MIXLORA_PROJECT(NQ_, DROP_, 8); \
+    else MIXLORA_PROJECT(NQ_, DROP_, (NQ_ > 2 ? 8 : 16));  \
+  } while (0)
   if (drop.thr) {
-    if (a.r <= 16) MIXLORA_PROJECT(1, true);
-    else if (a.r <= 32) MIXLORA_PROJECT(2, true);
-    else MIXLORA_PROJECT(4, true);
+    if (a.r <= 16) MIXLORA_PROJECT_W(1, true);
+    else if (a.r <= 32) MIXLORA_PROJECT_W(2, true);
+    else MIXLORA_PROJECT_W(4, true);
   } else {
-    if (a.r <= 16) MIXLORA_PROJECT(1, false);
-    else if (a.r <= 32) MIXLORA_PROJECT(2, false);
-    else MIXLORA_PROJECT(4, false);
+    if (a.r <= 16) MIXLORA_PROJECT_W(1, false);
+    else if (a.r <= 32) MIXLORA_PROJECT_W(2, false);
+    else MIXLORA_PROJECT_W(4, false);
   }
 #undef MIXLORA_PROJECT
+#undef MIXLORA_PROJECT_W
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  if (a.S > 1)
+    hipLaunchKernelGGL(project_finish_kernel, dim3((unsigned)(((int64_t)a.T * a.r + 255) / 256)), dim3(256), 0, st, a);
   if (slot >= 0) prof_mark_end(slot, st, 0.0);
   return hipGetLastError();
 }
@@ -240,6 +395,17 @@ struct Frozen {
     return Q4Matrix{(const unsigned char *)q4->codes, (const bf16_t *)q4->scales, D.d_out, D.d_in, q4->group};
   }
 };
+
+Project project(const Layout &L, char *ws, const void *X, const void *Wq, const void *Wr, int T,
+                int K, int cols, size_t P, size_t PT) {
+  Project a{};
+  a.X = (const bf16_t *)X, a.Wq = (const bf16_t *)Wq, a.Wr = (const bf16_t *)Wr;
+  a.T = T, a.K = K, a.r = L.rp, a.cols = cols, a.ldT = L.ldT;
+  a.P = (float *)(ws + P), a.part = (float *)(ws + L.proj);
+  a.PT = (bf16_t *)(ws + PT), a.ext = (bf16_t *)(ws + L.ext), a.ext_B = (bf16_t *)(ws + L.ext_B);
+  a.offs = (int32_t *)(ws + L.offs);
+  return a;
+}
 
 int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B, const DropArgs &drop, const void *x,
             void *y, char *ws, size_t ws_bytes, hipStream_t st) {
@@ -279,8 +445,7 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
     HIP_TRY(launch_lowrank_add(dt, y, P, B, T, dn, r, D.lora_scale, st));
     return MIXLORA_OK;
   }
-  const Project pr{x, A, B, T, di, r, dn, L.ldT, D.lora_scale, P, ws + L.P_T, ws + L.ext, ws + L.ext_B, (int32_t *)(ws + L.offs)};
-  HIP_TRY(launch_project(pr, drop, st));
+  HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, dn, L.P, L.P_T), D.lora_scale, drop, st));
   GemmProblem p = problem(T, dn, y, 0, x, W, di);
   p.seg[1] = GemmSeg{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
   p.nseg = 2;
@@ -336,13 +501,11 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
     HIP_TRY(launch_group_outer(go, 2, part, L.partial_floats, st));
   } else {
     if (L.few_floats) {   // the forward has not kept the projection
-      const Project px{x, A, B, T, di, r, 0, L.ldT, s, P, ws + L.P_T, ws + L.ext, ws + L.ext_B, (int32_t *)(ws + L.offs)};
-      HIP_TRY(launch_project(px, drop, st));
+      HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), s, drop, st));
     }
     // (the term of dx is masked and scaled, the factor V of dA is not)
-    const Project pr{dy, ws + L.Bt, ws + L.At, T, dn, r, di, L.ldT, drop.thr ? s * drop.inv : s, V, ws + L.V_T, ws + L.ext,
-                     ws + L.ext_B, (int32_t *)(ws + L.offs)};
-    HIP_TRY(launch_project(pr, DropArgs{}, st));
+    HIP_TRY(launch_project(project(L, ws, dy, ws + L.Bt, ws + L.At, T, dn, di, L.V, L.V_T),
+                           drop.thr ? s * drop.inv : s, DropArgs{}, st));
     const GemmScratch gs{L.gemm_floats ? (float *)(ws + L.gemm_part) : nullptr, L.gemm_floats};
     const GemmSeg frozen{dy, W_T, dn, dn, dn}, term{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
     GemmProblem p = problem(T, di, dx, 0, dy, W_T, dn);
@@ -362,9 +525,9 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
     }
     const GomJob go[2] = {
-        GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 3, drop},
-        GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, 3, DropArgs{}}};
-    HIP_TRY(launch_group_outer_mfma(go, 2, part, L.partial_floats, st));
+        GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, drop},
+        GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, DropArgs{}}};
+    HIP_TRY(launch_adapter_sums(go, 2, part, L.partial_floats, st));
   }
   if (L.rp != D.r) {
     const RelayoutJob jobs[2] = {job_rank_resize(dA, dA_user, 1, L.rp, D.r, di, true),

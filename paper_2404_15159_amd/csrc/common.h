@@ -423,13 +423,16 @@ struct GomJob {
   const int32_t *offs, *pair_of_row;
   int G, r, C, k, rows, ldT, alike, layout_qc;
   float scale;
-  int pieces;      // 3: smallT is [3][r][ldT], three bf16 pieces of an fp32 factor (of every job of a launch); else one
-  DropArgs drop;   // three pieces only: elements of wide that count as zeros (their factor belongs into scale)
+  DropArgs drop;   // launch_adapter_sums: elements of wide that count as zeros (their factor belongs into scale)
 };
 constexpr int GOM_MAX_JOBS = 8;
 hipError_t launch_group_outer_mfma(const GomJob *jobs, int njobs, float *partials, size_t partial_floats,
                                    hipStream_t st);
 size_t group_outer_mfma_partial_floats(int G, int r, int C, int rows, int alike);
+// Sums over all rows as one group (G = 1, no gather) with smallT [3][r][ldT]: an fp32 factor in three bf16 pieces, none of
+// whose bits is lost.
+hipError_t launch_adapter_sums(const GomJob *jobs, int njobs, float *partials, size_t partial_floats, hipStream_t st);
+size_t adapter_sums_partial_floats(int r, int C, int rows);
 // a per-row rank-r factor: (w_row or 1) * src[(by_token ? t(row) : row), e(row)*r + q], as bf16 at
 // outT[q, row] (pitch ldT) or in fp32 storage at outT[row, q]
 struct GatherJob {

@@ -169,16 +169,19 @@ struct GomBatch {
   int njobs;
 };
 
-// PIECES: smallT holds the factor in that many bf16 pieces ([piece][r][ldT]), whose products with the wide
-// rows go into one sum.  DROP: of a job with drop.thr != 0, the elements of wide that the generator drops
-// count as zeros (wide row = generator row).  Either only adds arithmetic to a step that waits for memory.
+// PIECES == 3 (launch_adapter_sums): smallT holds the factor in three bf16 pieces ([piece][r][ldT]), whose products with
+// the wide rows go into one sum; and the four waves take the 16-row steps of the same 256 columns in turn and add their
+// sums in LDS, so that few rows still fill the chip and a slice of the rows leaves a quarter of the partial sums.
+// DROP: of a job with drop.thr != 0, the elements of wide that the generator drops count as zeros (wide row =
+// generator row).
 template <int NQ, int PIECES = 1, bool DROP = false>
 __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(GomBatch batch) {
+  constexpr bool BY_ROWS = PIECES == 3;
   int ji = 0;
   while (ji + 1 < batch.njobs && batch.x0[ji + 1] <= (int)blockIdx.x) ji++;
   const GomJob &J = batch.job[ji];
   const int G = J.G, r = J.r, C = J.C, ldT = J.ldT, nsplit = batch.nsplit[ji], nrows = J.rows, k = J.k;
-  const int cgs = (C + 1023) >> 10, at = blockIdx.x - batch.x0[ji];
+  const int cgs = BY_ROWS ? (C + 255) >> 8 : (C + 1023) >> 10, at = blockIdx.x - batch.x0[ji];
   const int cg = at % cgs, g = at / cgs % G, sp = at / cgs / G;
   const bf16_t *__restrict__ smallT = reinterpret_cast<const bf16_t *>(J.smallT);
   const bf16_t *__restrict__ wide = reinterpret_cast<const bf16_t *>(J.wide);
@@ -191,8 +194,8 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
   const int per = (nsteps + nsplit - 1) / nsplit;
   const int st_lo = sp * per;
   const int st_hi = st_lo + per < nsteps ? st_lo + per : nsteps;
-  const int c0 = (cg * 4 + wave) * (32 * GOM_CB);
-  if (c0 >= C) return;   // whole wave out of range (no barriers in this kernel)
+  const int c0 = (BY_ROWS ? cg : cg * 4 + wave) * (32 * GOM_CB);
+  if (!BY_ROWS && c0 >= C) return;   // whole wave out of range (no barriers in this form)
   int ccol = c0 + 8 * l31;
   if (ccol >= C) ccol = C - 8;
   f32x16_t acc[GOM_CB][NQ];
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
   DropKey key;
   if constexpr (DROP) key = drop_key(J.drop);
   auto walk = [&](auto gather) {
-  for (int st = st_lo; st < st_hi; st++) {
+  for (int st = BY_ROWS ? st_lo + wave : st_lo; st < st_hi; st += BY_ROWS ? 4 : 1) {
     const int rbase = base + st * 16 + hi * 8;
     bf16x8_t bq[PIECES][NQ];
 #pragma unroll
@@ -240,6 +243,13 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
           bq[pc][j][p] = (qv & (row >= lo) & (row < hi_)) ? bq[pc][j][p] : (bf16_t)0.f;
       }
     }
+    if constexpr (BY_ROWS) {
+      if (st == nsteps - 1) {   // (a row past the last one is that row again: infinite times zero would be NaN)
+#pragma unroll
+        for (int p = 0; p < 8; p++)
+          if (rbase + p >= hi_) wrow[p] = bf16x8_t{};
+      }
+    }
     if constexpr (DROP) {
       if (J.drop.thr) {
 #pragma unroll
@@ -262,6 +272,37 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
   };
   if (pair_of_row) walk(std::true_type{});   // (decided outside the loop)
   else walk(std::false_type{});
+  if constexpr (BY_ROWS) {   // waves 2 and 3 into 0 and 1, then 1 into 0
+    extern __shared__ __align__(16) float gom_red[];   // [2][GOM_CB][NQ][4][64][4]
+#pragma unroll
+    for (int half = 2; half >= 1; half--) {
+      f32x4_t *mine = reinterpret_cast<f32x4_t *>(gom_red) + ((wave & (half - 1)) * GOM_CB * NQ * 4) * 64 + lane;
+      if (half == 1) __syncthreads();   // the sums of the first round are behind everybody
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int b = 0; b < GOM_CB; b++)
+#pragma unroll
+          for (int j = 0; j < NQ; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+              mine[((b * NQ + j) * 4 + i) * 64] = f32x4_t{acc[b][j][4 * i], acc[b][j][4 * i + 1], acc[b][j][4 * i + 2], acc[b][j][4 * i + 3]};
+      }
+      __syncthreads();
+      if (wave < half) {
+#pragma unroll
+        for (int b = 0; b < GOM_CB; b++)
+#pragma unroll
+          for (int j = 0; j < NQ; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+              const f32x4_t v = mine[((b * NQ + j) * 4 + i) * 64];
+#pragma unroll
+              for (int u = 0; u < 4; u++) acc[b][j][4 * i + u] += v[u];
+            }
+      }
+    }
+    if (wave != 0) return;
+  }
   const float scale = J.scale;
 #pragma unroll
   for (int j = 0; j < NQ; j++) {
@@ -396,27 +437,74 @@ hipError_t launch_group_outer_mfma(const GomJob *jobs, int njobs, float *partial
     n = m > n ? m : n;
   }
   if (used > partial_floats) return hipErrorInvalidValue;
-  bool three = false, drop = false;
-  for (int i = 0; i < njobs; i++) {
-    three |= jobs[i].pieces == 3;
-    drop |= jobs[i].drop.thr != 0;
-  }
-  for (int i = 0; i < njobs; i++)   // one instance for all jobs
-    if ((jobs[i].pieces == 3) != three || (drop && !three)) return hipErrorInvalidValue;
-#define MIXLORA_GOM(...) hipLaunchKernelGGL((group_outer_mfma_kernel<__VA_ARGS__>), dim3(x), dim3(256), 0, st, b)
-  if (rmax <= 32) {
-    if (!three) MIXLORA_GOM(1);
-    else if (!drop) MIXLORA_GOM(1, 3);
-    else MIXLORA_GOM(1, 3, true);
-  } else {
-    if (!three) MIXLORA_GOM(2);
-    else if (!drop) MIXLORA_GOM(2, 3);
-    else MIXLORA_GOM(2, 3, true);
-  }
-#undef MIXLORA_GOM
+  if (rmax <= 32) hipLaunchKernelGGL(group_outer_mfma_kernel<1>, dim3(x), dim3(256), 0, st, b);
+  else hipLaunchKernelGGL(group_outer_mfma_kernel<2>, dim3(x), dim3(256), 0, st, b);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 0) return e;   // unsplit rows: the kernel wrote the results
   hipLaunchKernelGGL(group_outer_reduce_kernel, dim3((unsigned)((n + 255) / 256), njobs), dim3(256), 0, st, b);
+  return hipGetLastError();
+}
+
+// Row slices of a job of two: two workgroups per CU, at least 64 rows each.
+static int adapter_splits(int C, int rows) {
+  int s = 256 / ((C + 255) / 256);
+  if (s > 32) s = 32;
+  if (s > rows / 64) s = rows / 64;
+  return s < 1 ? 1 : s;
+}
+size_t adapter_sums_partial_floats(int r, int C, int rows) {
+  const int s = adapter_splits(C, rows);
+  return s > 1 ? (size_t)s * r * C : 0;
+}
+hipError_t launch_adapter_sums(const GomJob *jobs, int njobs, float *partials, size_t partial_floats, hipStream_t st) {
+  if (njobs < 1 || njobs > GOM_MAX_JOBS) return hipErrorInvalidValue;
+  GomBatch b{};
+  b.njobs = njobs;
+  size_t used = 0;
+  int x = 0, rmax = 0;
+  bool drop = false;
+  int64_t n = 0;
+  for (int i = 0; i < njobs; i++) {
+    const GomJob &J = jobs[i];
+    if (J.G != 1 || J.pair_of_row || J.C % 8) return hipErrorInvalidValue;
+    b.job[i] = J;
+    b.nsplit[i] = adapter_splits(J.C, J.rows);
+    b.partial[i] = partials + used;
+    used += adapter_sums_partial_floats(J.r, J.C, J.rows);
+    b.x0[i] = x;
+    x += (J.C + 255) / 256 * b.nsplit[i];
+    rmax = J.r > rmax ? J.r : rmax;
+    drop |= J.drop.thr != 0;
+    const int64_t m = b.nsplit[i] > 1 ? (int64_t)J.r * J.C : 0;
+    n = m > n ? m : n;
+  }
+  if (used > partial_floats) return hipErrorInvalidValue;
+  const int slot = prof_on() ? prof_mark_begin(PROF_GRAD_SUMS, st) : -1;
+#define MIXLORA_ADAPTER_SUMS(NQ_, DROP_)                                                                              \
+  do {                                                                                                                \
+    constexpr size_t lds_ = (size_t)2 * GOM_CB * NQ_ * 4 * 64 * 16;                                                   \
+    static const hipError_t e_ = hipFuncSetAttribute((const void *)group_outer_mfma_kernel<NQ_, 3, DROP_>,            \
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_);          \
+    if (e_ != hipSuccess) return e_;                                                                                  \
+    hipLaunchKernelGGL((group_outer_mfma_kernel<NQ_, 3, DROP_>), dim3(x), dim3(256), lds_, st, b);                    \
+  } while (0)
+  if (rmax <= 32) {
+    if (drop) MIXLORA_ADAPTER_SUMS(1, true);
+    else MIXLORA_ADAPTER_SUMS(1, false);
+  } else {
+    if (drop) MIXLORA_ADAPTER_SUMS(2, true);
+    else MIXLORA_ADAPTER_SUMS(2, false);
+  }
+#undef MIXLORA_ADAPTER_SUMS
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (n > 0)
+    hipLaunchKernelGGL(group_outer_reduce_kernel, dim3((unsigned)((n + 255) / 256), njobs), dim3(256), 0, st, b);
+  if (slot >= 0) {
+    double bytes = 0;
+    for (int i = 0; i < njobs; i++) bytes += 2.0 * jobs[i].rows * jobs[i].C;
+    prof_mark_end(slot, st, bytes);
+  }
   return hipGetLastError();
 }
 

@@ -65,7 +65,8 @@ def test_quantize_refusals(back):
 def test_workspace_sizes():
     for fn in (lambda d, b: B.mixlora_q4_linear_workspace_bytes(d, 64, b), B.mixlora_lora_dropout_workspace_bytes):
         assert 0 < fn(lin(), False) <= fn(lin(), True)
-        for bad in (lin(T=0), lin(T=1 << 24), lin(d_in=60), lin(d_out=4), lin(r=0), lin(r=65), lin(dtype=3)):
+        for bad in (lin(T=0), lin(T=1 << 24), lin(d_in=60), lin(d_out=4), lin(r=0), lin(r=65), lin(dtype=3),
+                    lin(d_in=1 << 27), lin(d_out=1 << 27)):
             assert fn(bad, False) == 0 and fn(bad, True) == 0
     assert B.mixlora_q4_linear_workspace_bytes(lin(), 96, True) == 0
     # the largest the limits allow stay positive 64-bit numbers
