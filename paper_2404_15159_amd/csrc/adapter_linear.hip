@@ -525,8 +525,8 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
     }
     const GomJob go[2] = {
-        GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, drop},
-        GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, DropArgs{}}};
+        GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 0, drop},
+        GomJob{ws + L.P_T, dy, dB, offs, nullptr, 1, r, dn, 1, T, L.ldT, 2, 0, s, 0, DropArgs{}}};
     HIP_TRY(launch_adapter_sums(go, 2, part, L.partial_floats, st));
   }
   if (L.rp != D.r) {

@@ -423,6 +423,7 @@ struct GomJob {
   const int32_t *offs, *pair_of_row;
   int G, r, C, k, rows, ldT, alike, layout_qc;
   float scale;
+  int r_all;       // launch_adapter_sums: rank entries of smallT and out, of which a job may hold some (0: r)
   DropArgs drop;   // launch_adapter_sums: elements of wide that count as zeros (their factor belongs into scale)
 };
 constexpr int GOM_MAX_JOBS = 8;

@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 #pragma unroll
       for (int j = 0; j < NQ; j++) {
         const int q = j * 32 + l31;
-        bq[pc][j] = *reinterpret_cast<const bf16x8_t *>(smallT + (int64_t)(pc * r + (q < r ? q : 0)) * ldT + rbase);
+        bq[pc][j] = *reinterpret_cast<const bf16x8_t *>(smallT + (int64_t)(pc * J.r_all + (q < r ? q : 0)) * ldT + rbase);
       }
     // rows read in place are read exactly once per step: a streaming (non-temporal) load keeps them from
     // displacing the gathered rows and partial results other kernels reuse (the sums over the d_ff-wide
@@ -327,9 +327,9 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
                     make_float4(scale * acc[4][j][gg * 4 + m], scale * acc[5][j][gg * 4 + m],
                                 scale * acc[6][j][gg * 4 + m], scale * acc[7][j][gg * 4 + m]);
               } else {
-                float *o = out + ((int64_t)g * C + c) * r + q;
+                float *o = out + ((int64_t)g * C + c) * J.r_all + q;
 #pragma unroll
-                for (int b = 0; b < GOM_CB; b++) o[(int64_t)b * r] = scale * acc[b][j][gg * 4 + m];
+                for (int b = 0; b < GOM_CB; b++) o[(int64_t)b * J.r_all] = scale * acc[b][j][gg * 4 + m];
               }
             }
           }
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256) void group_outer_reduce_kernel(GomBatch batch)
     J.out[i] = acc;
   } else {
     const int c = (int)(i % C), q = (int)(i / C % r), g = (int)(i / ((int64_t)C * r));
-    J.out[((int64_t)g * C + c) * r + q] = acc;
+    J.out[((int64_t)g * C + c) * J.r_all + q] = acc;
   }
 }
 
@@ -427,6 +427,7 @@ hipError_t launch_group_outer_mfma(const GomJob *jobs, int njobs, float *partial
   for (int i = 0; i < njobs; i++) {
     const GomJob &J = jobs[i];
     b.job[i] = J;
+    b.job[i].r_all = J.r;
     b.nsplit[i] = gom_splits(J.G, J.C, J.rows, J.alike);
     b.partial[i] = partials + used;
     used += group_outer_mfma_partial_floats(J.G, J.r, J.C, J.rows, J.alike);
@@ -456,12 +457,29 @@ size_t adapter_sums_partial_floats(int r, int C, int rows) {
   const int s = adapter_splits(C, rows);
   return s > 1 ? (size_t)s * r * C : 0;
 }
-hipError_t launch_adapter_sums(const GomJob *jobs, int njobs, float *partials, size_t partial_floats, hipStream_t st) {
-  if (njobs < 1 || njobs > GOM_MAX_JOBS) return hipErrorInvalidValue;
+hipError_t launch_adapter_sums(const GomJob *all, int nall, float *partials, size_t partial_floats, hipStream_t st) {
+  if (nall < 1 || nall > GOM_MAX_JOBS / 2) return hipErrorInvalidValue;
+  GomJob jobs[GOM_MAX_JOBS];
+  int njobs = 0;
+  for (int i = 0; i < nall; i++) {
+    jobs[njobs] = all[i];
+    jobs[njobs].r_all = all[i].r;
+    // More than 32 rank entries are two jobs: one wave's sums for 64 do not fit its registers, and twice the workgroups are
+    // worth reading the wide rows twice (rank 64, 4096 x 4096: a step of 333 tokens 139 -> 129 us, 8192 538 -> 535).
+    if (all[i].r > 32) {
+      jobs[njobs].r = 32;
+      jobs[njobs + 1] = jobs[njobs];
+      GomJob &J = jobs[++njobs];
+      J.r = all[i].r - 32;
+      J.smallT = (const bf16_t *)J.smallT + (int64_t)32 * J.ldT;
+      J.out += J.layout_qc ? (int64_t)32 * J.C : 32;
+    }
+    njobs++;
+  }
   GomBatch b{};
   b.njobs = njobs;
   size_t used = 0;
-  int x = 0, rmax = 0;
+  int x = 0;
   bool drop = false;
   int64_t n = 0;
   for (int i = 0; i < njobs; i++) {
@@ -473,28 +491,20 @@ hipError_t launch_adapter_sums(const GomJob *jobs, int njobs, float *partials, s
     used += adapter_sums_partial_floats(J.r, J.C, J.rows);
     b.x0[i] = x;
     x += (J.C + 255) / 256 * b.nsplit[i];
-    rmax = J.r > rmax ? J.r : rmax;
     drop |= J.drop.thr != 0;
     const int64_t m = b.nsplit[i] > 1 ? (int64_t)J.r * J.C : 0;
     n = m > n ? m : n;
   }
   if (used > partial_floats) return hipErrorInvalidValue;
   const int slot = prof_on() ? prof_mark_begin(PROF_GRAD_SUMS, st) : -1;
-#define MIXLORA_ADAPTER_SUMS(NQ_, DROP_)                                                                              \
+#define MIXLORA_ADAPTER_SUMS(DROP_)                                                                                   \
   do {                                                                                                                \
-    constexpr size_t lds_ = (size_t)2 * GOM_CB * NQ_ * 4 * 64 * 16;                                                   \
-    static const hipError_t e_ = hipFuncSetAttribute((const void *)group_outer_mfma_kernel<NQ_, 3, DROP_>,            \
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_);          \
-    if (e_ != hipSuccess) return e_;                                                                                  \
-    hipLaunchKernelGGL((group_outer_mfma_kernel<NQ_, 3, DROP_>), dim3(x), dim3(256), lds_, st, b);                    \
+    constexpr size_t lds_ = (size_t)2 * GOM_CB * 4 * 64 * 16;                                                         \
+    static_assert(lds_ <= 65536, "no attribute needed");                                                              \
+    hipLaunchKernelGGL((group_outer_mfma_kernel<1, 3, DROP_>), dim3(x), dim3(256), lds_, st, b);                      \
   } while (0)
-  if (rmax <= 32) {
-    if (drop) MIXLORA_ADAPTER_SUMS(1, true);
-    else MIXLORA_ADAPTER_SUMS(1, false);
-  } else {
-    if (drop) MIXLORA_ADAPTER_SUMS(2, true);
-    else MIXLORA_ADAPTER_SUMS(2, false);
-  }
+  if (drop) MIXLORA_ADAPTER_SUMS(true);
+  else MIXLORA_ADAPTER_SUMS(false);
 #undef MIXLORA_ADAPTER_SUMS
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -21,54 +21,81 @@ __device__ __forceinline__ float q4_scale(uint32_t most_bits) {
   if (6.f * __uint_as_float(b) < most) b += LOW + 1;   // (the quotient was rounded down onto such a number)
   return __uint_as_float(b);
 }
+// (a bisection: the midpoints in order are 1/4, 3/4, 5/4, 7/4, 5/2, 7/2, 5, and a tie goes up at every second one)
 __device__ __forceinline__ uint32_t q4_code(float w, float s) {
   const float a = fabsf(w);
-  uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) +
-               (a >= 3.5f * s) + (a > 5.f * s);
-  if (s == 0.f) c = 0;
-  return c | (w < 0.f && c ? 8u : 0u);
+  const bool b2 = a >= 1.75f * s;
+  const bool b1 = a >= (b2 ? 3.5f * s : 0.75f * s);
+  const bool b0 = a > (b2 ? (b1 ? 5.f * s : 2.5f * s) : (b1 ? 1.25f * s : 0.25f * s));
+  const uint32_t c = (b2 ? 4u : 0u) + (b1 ? 2u : 0u) + (b0 ? 1u : 0u);
+  return s == 0.f ? 0u : c | (w < 0.f && c ? 8u : 0u);
 }
 
-// Bound by reading W once.  A wavefront owns a tile, a lane eight consecutive inputs of a row four times
-// over; 16 lanes share a row, so a group's largest magnitude is a butterfly over 4, 8 or 16 of them.
-template <typename E>
-__global__ __launch_bounds__(256) void q4_quantize_kernel(const E *__restrict__ W, int n, int K, int group,
+// Bound by reading W once.  A wavefront owns a tile; four neighbouring lanes have 64 bytes of a row between them (in bf16),
+// four times over, and what a lane has is what it writes: the 16 bytes of its row and quarter.
+template <typename E, int PER>
+__global__ __launch_bounds__(256) void q4_quantize_kernel(const E *__restrict__ W, int n, int K,
                                                           unsigned char *__restrict__ codes,
                                                           bf16_t *__restrict__ scales) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, i = lane >> 2, h = lane & 3;
   const int64_t kt = q4_col_blocks(K), tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (tile >= q4_row_blocks(n) * kt) return;
-  const int row0 = (int)(tile / kt) * Q4_ROWS, k0 = (int)(tile % kt) * Q4_COLS;
-  const int j = lane & 15, k = k0 + 8 * j, per = Q4_COLS / group, lanes = group / 8;
+  const int row = (int)(tile / kt) * Q4_ROWS + i, k0 = (int)(tile % kt) * Q4_COLS;
+  const bool whole = row < n && k0 + Q4_COLS <= K;
+  const E *src = W + (int64_t)(row < n ? row : n - 1) * K;
   Vec8<E> v[4];
 #pragma unroll
-  for (int p = 0; p < 4; p++) {
-    const int row = row0 + p * 4 + (lane >> 4);
-    v[p].load(W + (int64_t)(row < n ? row : n - 1) * K + (k < K ? k : 0));
+  for (int b = 0; b < 4; b++) {
+    const int k = k0 + 32 * b + 8 * h;
+    v[b].load(src + (k < K ? k : 0));
   }
+  float w[4][8];
+  uint32_t most[4];
 #pragma unroll
-  for (int p = 0; p < 4; p++) {
-    const int i = p * 4 + (lane >> 4);
-    const bool in = row0 + i < n && k < K;   // K is a multiple of 8
-    float w[8];
-    uint32_t most = 0;
+  for (int b = 0; b < 4; b++) {
+    const bool in = whole || (row < n && k0 + 32 * b + 8 * h < K);   // K is a multiple of 8
+    most[b] = 0;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-      w[e] = in ? v[p].get(e) : 0.f;
-      const uint32_t b = __float_as_uint(w[e]) & 0x7fffffffu;
-      most = b > most ? b : most;
+      w[b][e] = in ? v[b].get(e) : 0.f;
+      const uint32_t bits = __float_as_uint(w[b][e]) & 0x7fffffffu;
+      most[b] = bits > most[b] ? bits : most[b];
     }
-    for (int m = 1; m < lanes; m <<= 1) {
-      const uint32_t o = __shfl_xor(most, m);
-      most = o > most ? o : most;
-    }
-    const float s = q4_scale(most);
-    uint32_t word = 0;
-#pragma unroll
-    for (int e = 0; e < 8; e++) word |= q4_code(w[e], s) << (4 * e);
-    *reinterpret_cast<uint32_t *>(codes + tile * Q4_TILE_BYTES + 16 * (16 * (j & 3) + i) + 4 * (j >> 2)) = word;
-    if (j % lanes == 0) scales[(tile * Q4_ROWS + i) * per + j / lanes] = (bf16_t)s;
   }
+  uint32_t word[4];
+#pragma unroll
+  for (int g = 0; g < PER; g++) {
+    constexpr int STEPS = 4 / PER;
+    uint32_t m = most[g * STEPS];
+#pragma unroll
+    for (int b = 1; b < STEPS; b++) m = most[g * STEPS + b] > m ? most[g * STEPS + b] : m;
+    uint32_t o = __builtin_amdgcn_update_dpp(0, m, 0xb1, 0xf, 0xf, true);   // quad_perm 1 0 3 2
+    m = o > m ? o : m;
+    o = __builtin_amdgcn_update_dpp(0, m, 0x4e, 0xf, 0xf, true);            // quad_perm 2 3 0 1
+    m = o > m ? o : m;
+    const float s = q4_scale(m);
+#pragma unroll
+    for (int b = g * STEPS; b < (g + 1) * STEPS; b++) {
+      word[b] = 0;
+#pragma unroll
+      for (int e = 0; e < 8; e++) word[b] |= q4_code(w[b][e], s) << (4 * e);
+    }
+    if (h == 0) scales[(tile * Q4_ROWS + i) * PER + g] = (bf16_t)s;
+  }
+  *reinterpret_cast<uint4 *>(codes + tile * Q4_TILE_BYTES + 16 * (16 * h + i)) = uint4{word[0], word[1], word[2], word[3]};
+}
+template <typename E>
+static hipError_t launch_quantize(const void *W, int n, int K, const mixlora_q4 &q, hipStream_t st) {
+  const int64_t tiles = q4_row_blocks(n) * q4_col_blocks(K);
+  const dim3 grid((unsigned)((tiles + 3) / 4)), block(256);
+#define MIXLORA_QUANTIZE(PER_)                                                                                 \
+  hipLaunchKernelGGL((q4_quantize_kernel<E, PER_>), grid, block, 0, st, (const E *)W, n, K, (unsigned char *)q.codes, \
+                     (bf16_t *)q.scales)
+  if (q.group == 128) MIXLORA_QUANTIZE(1);
+  else if (q.group == 64) MIXLORA_QUANTIZE(2);
+  else MIXLORA_QUANTIZE(4);
+#undef MIXLORA_QUANTIZE
+  return hipGetLastError();
 }
 
 // ---- and back ---------------------------------------------------------------------------------------
@@ -180,15 +207,9 @@ int mixlora_q4_quantize(const void *W, int32_t dtype, int32_t d_out, int32_t d_i
   if (rc) return rc;
   if (misaligned(W) || misaligned(q4->codes) || misaligned(q4->scales)) return MIXLORA_E_ALIGN;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const int64_t tiles = q4_row_blocks(d_out) * q4_col_blocks(d_in);
-  const dim3 grid((unsigned)((tiles + 3) / 4)), block(256);
-  if (dtype == MIXLORA_BF16)
-    hipLaunchKernelGGL(q4_quantize_kernel<bf16_t>, grid, block, 0, st, (const bf16_t *)W, d_out, d_in, q4->group,
-                       (unsigned char *)q4->codes, (bf16_t *)q4->scales);
-  else
-    hipLaunchKernelGGL(q4_quantize_kernel<float>, grid, block, 0, st, (const float *)W, d_out, d_in, q4->group,
-                       (unsigned char *)q4->codes, (bf16_t *)q4->scales);
-  return hipGetLastError() == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
+  const hipError_t e = dtype == MIXLORA_BF16 ? launch_quantize<bf16_t>(W, d_out, d_in, *q4, st)
+                                             : launch_quantize<float>(W, d_out, d_in, *q4, st);
+  return e == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
 }
 
 int mixlora_q4_dequantize(const mixlora_q4 *q4, int32_t d_out, int32_t d_in, int32_t transposed, void *W,
