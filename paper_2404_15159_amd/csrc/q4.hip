@@ -31,6 +31,34 @@ __device__ __forceinline__ uint32_t q4_code(float w, float s) {
   return s == 0.f ? 0u : c | (w < 0.f && c ? 8u : 0u);
 }
 
+// Eight codes of bf16 weights by the hardware's conversion (nearest, ties to even) of the quotients.  It needs them right at
+// the midpoints only: w has 8 significant bits and midpoint x scale at most 9, so they differ by 2^-9 or not at all, and in
+// that case the corrected quotient is the midpoint itself (w - q s is exact, so q + (w - q s) / s is rounded once, and the
+// midpoint needs no rounding).  For 24 bits that does not hold.
+__device__ __forceinline__ uint32_t q4_codes_bf16(const float (&w)[8], float s) {
+  const float r = __builtin_amdgcn_rcpf(s);
+  uint32_t word = 0;
+  float q[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) {
+    const float q0 = w[e] * r;
+    q[e] = fmaf(fmaf(-q0, s, w[e]), r, q0);
+  }
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, q[0], q[1], 1.f, 0);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, q[2], q[3], 1.f, 1);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, q[4], q[5], 1.f, 2);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, q[6], q[7], 1.f, 3);
+  word &= 0x77777777u | ((word | word >> 1 | word >> 2) & 0x11111111u) << 3;   // a magnitude of 0 has no sign
+  return s > 0.f ? word : 0u;
+}
+template <typename E> __device__ __forceinline__ uint32_t q4_codes(const float (&w)[8], float s) {
+  uint32_t word = 0;
+#pragma unroll
+  for (int e = 0; e < 8; e++) word |= q4_code(w[e], s) << (4 * e);
+  return word;
+}
+template <> __device__ __forceinline__ uint32_t q4_codes<bf16_t>(const float (&w)[8], float s) { return q4_codes_bf16(w, s); }
+
 // Bound by reading W once.  A wavefront owns a tile; four neighbouring lanes have 64 bytes of a row between them (in bf16),
 // four times over, and what a lane has is what it writes: the 16 bytes of its row and quarter.
 template <typename E, int PER>
@@ -75,11 +103,7 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const E *__restrict__ 
     m = o > m ? o : m;
     const float s = q4_scale(m);
 #pragma unroll
-    for (int b = g * STEPS; b < (g + 1) * STEPS; b++) {
-      word[b] = 0;
-#pragma unroll
-      for (int e = 0; e < 8; e++) word[b] |= q4_code(w[b][e], s) << (4 * e);
-    }
+    for (int b = g * STEPS; b < (g + 1) * STEPS; b++) word[b] = q4_codes<E>(w[b], s);
     if (h == 0) scales[(tile * Q4_ROWS + i) * PER + g] = (bf16_t)s;
   }
   *reinterpret_cast<uint4 *>(codes + tile * Q4_TILE_BYTES + 16 * (16 * h + i)) = uint4{word[0], word[1], word[2], word[3]};

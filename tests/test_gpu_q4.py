@@ -79,6 +79,44 @@ def test_quantize_and_back(n, K, group, dtype):
             assert np.array_equal(got.T if tr else got, want, equal_nan=True), (od, tr)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("e", [-99, -20, 0, 60])
+def test_every_bf16_weight_under_every_scale(e, dtype):
+    """All bf16 weights of six binades below 6 s, of both signs, under each of the 32 scales of a binade: the whole input
+    range of a code, midpoints and their neighbours among them.  One weight of 6 s per group fixes the scale.  In
+    fp32 also the next numbers beside each of them."""
+    rows = []
+    for m in range(32, 64):
+        s = np.float64(m) / 32 * 2.0 ** e
+        v = np.arange(128, 256)[None, :] * 2.0 ** np.arange(-11, -4)[:, None]      # 8-bit significands
+        v = (v.reshape(-1) * 2.0 ** e).astype(np.float32)
+        v = v[v <= 6 * s]
+        if dtype == "f32":
+            v = np.concatenate([v, np.nextafter(v, np.float32(0)), np.nextafter(v, np.float32(3e38))])
+            v = v[v <= 6 * s]
+        v = np.concatenate([v, -v])
+        v = np.resize(v, -(-len(v) // 31) * 31).reshape(-1, 31)
+        rows.append(np.concatenate([np.full((len(v), 1), 6 * s), v], 1).reshape(-1))
+    K = -(-max(len(r) for r in rows) // 8) * 8
+    W = np.stack([np.resize(r, K) for r in rows]).astype(np.float32)
+    W[:, ::32] = W[:, :1]
+    n = 32
+    s = np.float64(np.arange(32, 64)) / 32 * 2.0 ** e
+    mids = (orc.LEVELS[1:] + orc.LEVELS[:-1]) / 2 * s[:, None]
+    a = np.abs(W.astype(np.float64))
+    c = sum((a >= mids[:, i:i + 1]) if i % 2 else (a > mids[:, i:i + 1]) for i in range(7))   # ties to the even code
+    want = orc.LEVELS[c] * s[:, None] * np.sign(W)
+    codes = torch.empty(B.mixlora_q4_code_bytes(n, K), dtype=torch.uint8, device=DEV)
+    scales = torch.empty(B.mixlora_q4_scale_bytes(n, K, 32) // 2, dtype=torch.bfloat16, device=DEV)
+    q = B.make_q4(codes, scales, 32)
+    out = torch.empty((n, K), dtype=torch.float32, device=DEV)
+    B.mixlora_q4_quantize(dev(W, dtype), CODE[dtype], n, K, q)
+    B.mixlora_q4_dequantize(q, n, K, False, out, B.F32)
+    torch.cuda.synchronize()
+    assert dtype == "f32" or np.array_equal(rounded(W, "bf16"), W)
+    assert np.array_equal(out.cpu().numpy().astype(np.float64), want)
+
+
 def check(name, got, want, sums, terms, dtype):
     """A result is a sum of `terms` products in fp32, each step off by half a step of fp32 relative to the
     sum of magnitudes (2^-24; twice that, since the matrix pipe may cut instead of round), and one rounding
