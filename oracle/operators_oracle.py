@@ -29,18 +29,22 @@ def nearest_code(w, s):
 
 
 def quantize(W, group):
-    """codes [n, K] (0-15) and scales [n, groups]."""
+    """codes [n, K] (0-15) and scales [n, groups]; nearest_code for all weights at once."""
     n, K = W.shape
     G = -(-K // group)
-    codes, scales = np.zeros((n, K), np.uint8), np.zeros((n, G))
     W = W.astype(np.float64)
-    for i in range(n):
-        for g in range(G):
-            w = W[i, g * group:(g + 1) * group]
-            most = np.max(np.abs(w)) if not np.isnan(w).any() else np.nan
-            scales[i, g] = group_scale(most)
-            codes[i, g * group:(g + 1) * group] = [nearest_code(v, scales[i, g]) for v in w]
-    return codes, scales
+    padded = np.zeros((n, G * group))
+    padded[:, :K] = W
+    most = np.abs(padded).reshape(n, G, group).max(2)      # NaN where one is
+    scales = np.array([group_scale(m) for m in most.reshape(-1)]).reshape(n, G)
+    s = np.repeat(scales, group, axis=1)[:, :K]
+    codes, off = np.zeros((n, K), np.uint8), np.full((n, K), np.inf)
+    with np.errstate(invalid="ignore"):
+        for c in (0, 2, 4, 6, 1, 3, 5, 7):                  # even codes first: a tie stays with them
+            d = np.abs(np.abs(W) - LEVELS[c] * s)
+            codes, off = np.where(d < off, c, codes).astype(np.uint8), np.minimum(d, off)
+        codes[~(s > 0)] = 0
+        return np.where((W < 0) & (codes > 0), codes + 8, codes).astype(np.uint8), scales
 
 
 def values(codes, scales, group):
@@ -53,13 +57,12 @@ def pack(codes, scales, group):
     n, K = codes.shape
     nt, kt, per = -(-n // 16), -(-K // 128), 128 // group
     out, sc = np.zeros(nt * kt * 1024, np.uint8), np.zeros(nt * kt * 16 * per)
-    for i in range(n):
-        for k in range(K):
-            b, h, e = k % 128 // 32, k % 32 // 8, k % 8
-            at = (i // 16 * kt + k // 128) * 1024 + 16 * (16 * h + i % 16) + 4 * b + e // 2
-            out[at] |= codes[i, k] << (4 * (e % 2))
-        for g in range(scales.shape[1]):
-            sc[((i // 16 * kt + g // per) * 16 + i % 16) * per + g % per] = scales[i, g]
+    i, k = np.arange(n)[:, None], np.arange(K)[None, :]
+    b, h, e = k % 128 // 32, k % 32 // 8, k % 8
+    at = (i // 16 * kt + k // 128) * 1024 + 16 * (16 * h + i % 16) + 4 * b + e // 2
+    np.bitwise_or.at(out, at, codes << (4 * (e % 2)).astype(np.uint8))
+    g = np.arange(scales.shape[1])[None, :]
+    sc[((i // 16 * kt + g // per) * 16 + i % 16) * per + g % per] = scales
     return out, sc
 
 
@@ -76,16 +79,19 @@ def philox(counter, key, rounds=7):
 
 
 def dropout_factors(T, width, p, seed, offset):
-    """[T, width]: 0 where an element is dropped, else the factor it gets."""
+    """[T, width]: 0 where an element is dropped, else the factor it gets; philox for all blocks at once."""
     thr = int(np.floor(float(np.float32(p)) * 65536.0 + 0.5))
-    out = np.zeros((T, width))
-    for t in range(T):
-        for c8 in range(-(-width // 8)):
-            w = philox((c8, t, offset & 0xFFFFFFFF, offset >> 32), (seed & 0xFFFFFFFF, seed >> 32))
-            for e in range(min(8, width - 8 * c8)):
-                if (w[e // 2] >> (16 * (e % 2)) & 0xFFFF) >= thr:
-                    out[t, 8 * c8 + e] = 65536.0 / (65536.0 - thr)
-    return out
+    u = np.uint64
+    low, half = u(0xFFFFFFFF), u(32)
+    t, c8 = np.meshgrid(np.arange(T, dtype=u), np.arange(-(-width // 8), dtype=u), indexing="ij")
+    c = [c8, t, np.full_like(t, u(offset & 0xFFFFFFFF)), np.full_like(t, u(offset >> 32))]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(7):
+        a, b = u(0xD2511F53) * c[0], u(0xCD9E8D57) * c[2]
+        c = [(b >> half) ^ c[1] ^ u(k[0]), b & low, (a >> half) ^ c[3] ^ u(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    bits = np.stack([w >> u(16 * h) & u(0xFFFF) for w in c for h in (0, 1)], axis=2)
+    return np.where(bits.reshape(T, -1)[:, :width] >= u(thr), 65536.0 / (65536.0 - thr), 0.0)
 
 
 # ---- LoRA linear ----------------------------------------------------------------------------------

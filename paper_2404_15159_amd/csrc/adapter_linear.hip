@@ -4,8 +4,8 @@
 // D' drops the same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen
 // product as an extra K segment, in three bf16 pieces that hold all of its 24 bits; the backward's, which has to
 // be masked with dropout, goes first and is masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as
-// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h), but for the forward of up to
-// 128 rows, which multiplies with the codes (q4_few.hip).
+// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h), but for the forward of few rows,
+// which multiplies with the codes (q4_few.hip).
 #include "common.h"
 #include "q4.h"
 #include "q4_few.h"
@@ -30,7 +30,7 @@ struct Layout {
   size_t W, fwd_end;
   size_t W_T, Bt, At, V, V_T, dx32, partials, padgA, padgB, bwd_end;
   size_t few;                             // partial sums of the few-rows product
-  size_t gemm_floats, partial_floats, few_floats;
+  size_t gemm_floats, partial_floats, few_floats, mid_floats;
 };
 
 size_t project_floats(int T, int K, int r);   // partial sums of a projection
@@ -63,10 +63,11 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   }
   L.xd = take(bf16 ? 0 : T * di * E);
   const size_t scratch = o;
-  // up to 128 rows in bf16 multiply with the codes themselves
+  // few rows in bf16 multiply with the codes themselves
   L.few_floats = q4 && bf16 ? q4_few_scratch_floats((int)dn, (int)di, (int)T, (int)r) : 0;
-  L.few = take(L.few_floats * 4);
-  L.W = take(q4 && !L.few_floats ? di * dn * E : 0);
+  L.mid_floats = q4 && bf16 && !L.few_floats && q4_mid_ok((int)dn, (int)di, (int)T) ? q4_mid_scratch_floats((int)dn, (int)di, (int)T) : 0;
+  L.few = take((L.few_floats + L.mid_floats) * 4);
+  L.W = take(q4 && !L.few_floats && !L.mid_floats ? di * dn * E : 0);
   L.fwd_end = o;
   o = scratch;
   L.W_T = take(di * dn * E);
@@ -118,10 +119,6 @@ int make_drop(const mixlora_dropout *d, DropArgs &out) {
     if (e_ != hipSuccess) return MIXLORA_E_HIP;         \
   } while (0)
 
-__global__ void set_offsets_kernel(int32_t *p, int T) {
-  if (threadIdx.x == 0) { p[0] = 0; p[1] = T; }
-}
-
 // fp32 storage: out = D(x), eight elements per thread
 __global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restrict__ x, float *__restrict__ out,
                                                           int64_t chunks, int per_row, DropArgs drop) {
@@ -135,14 +132,14 @@ __global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restric
   v.store(out + i * 8);
 }
 
-// out[t, c] = base[t, c] + (c of row t kept ? f * sum_q V[t, q] At[c, q] : 0), rounded once.  Four rows of
-// eight columns per thread.
-constexpr int MLA_ROWS = 4;
-template <typename E>
-__global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *__restrict__ base,
-                                                                 const float *__restrict__ V,
-                                                                 const E *__restrict__ At, E *__restrict__ out,
-                                                                 int T, int C, int r, float f, DropArgs drop) {
+// out[t, c] = base[t, c] + (c of row t kept ? f * sum_q V[t, q] At[c, q] : 0), rounded once (fp32 storage: base is out).
+// ROWS rows of eight columns per thread.  offs: all tokens are one group of the gradient sums.
+template <typename E, int ROWS>
+__global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *base, const float *__restrict__ V,
+                                                                 const E *__restrict__ At, E *out, int T, int C, int r,
+                                                                 float f, DropArgs drop, int32_t *offs) {
+  constexpr int MLA_ROWS = ROWS;
+  if (offs && blockIdx.x == 0 && threadIdx.x == 0) offs[0] = 0, offs[1] = T;
   const int cv = C / 8;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int chunk = (int)(id % cv), c0 = chunk * 8;
@@ -177,7 +174,7 @@ __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *__
 #pragma unroll
   for (int i = 0; i < MLA_ROWS; i++) {
     if (t0 + i >= T) break;
-    const uint32_t keep = drop_keep8(key, (uint32_t)(t0 + i), (uint32_t)chunk);
+    const uint32_t keep = drop.thr ? drop_keep8(key, (uint32_t)(t0 + i), (uint32_t)chunk) : 0xffu;
     Vec8<float> b;
     b.load(base + (int64_t)(t0 + i) * C + c0);
     Vec8<E> o;
@@ -188,11 +185,16 @@ __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *__
 }
 template <typename E>
 hipError_t launch_masked_add(const float *base, const float *V, const void *At, void *out, int T, int C, int r, float f,
-                             const DropArgs &drop, hipStream_t st) {
-  const int64_t threads = (int64_t)((T + MLA_ROWS - 1) / MLA_ROWS) * (C / 8);
+                             const DropArgs &drop, int32_t *offs, hipStream_t st) {
+  // four rows per thread read At a quarter as often; one where that leaves most of the chip without a workgroup
+  const bool four = (int64_t)T * (C / 8) >= 4 * 256 * 256;
+  const int64_t threads = (four ? (int64_t)(T + 3) / 4 : T) * (C / 8);
+  const dim3 grid((unsigned)((threads + 255) / 256)), block(256);
   const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
-  hipLaunchKernelGGL(masked_lowrank_add_kernel<E>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, base, V,
-                     (const E *)At, (E *)out, T, C, r, f, drop);
+  if (four)
+    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 4>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, f, drop, offs);
+  else
+    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 1>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, f, drop, offs);
   if (slot >= 0) prof_mark_end(slot, st, (double)T * C * (4 + sizeof(E)));
   return hipGetLastError();
 }
@@ -427,6 +429,12 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
     HIP_TRY(launch_q4_few(F.q4_matrix(D), a, drop, (float *)(ws + L.few), L.few_floats, st));
     return MIXLORA_OK;
   }
+  if (L.mid_floats) {
+    HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), D.lora_scale, drop, st));
+    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.lora_scale, (bf16_t *)y};
+    HIP_TRY(launch_q4_mid(F.q4_matrix(D), a, P, (float *)(ws + L.few), L.mid_floats, st));
+    return MIXLORA_OK;
+  }
   if (F.q4) {
     HIP_TRY(launch_q4_dequantize(F.q4_matrix(D), false, dt, ws + L.W, st));
     W = ws + L.W;
@@ -442,7 +450,7 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
     }
     const GemmProblem p[2] = {problem(T, dn, y, 0, x, W, di), problem(T, r, P, 1, xd, A, di)};
     HIP_TRY(launch_gemm(dt, p, 2, st));
-    HIP_TRY(launch_lowrank_add(dt, y, P, B, T, dn, r, D.lora_scale, st));
+    HIP_TRY(launch_masked_add<float>((const float *)y, P, B, y, T, dn, r, D.lora_scale, DropArgs{}, nullptr, st));
     return MIXLORA_OK;
   }
   HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, dn, L.P, L.P_T), D.lora_scale, drop, st));
@@ -490,12 +498,10 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       HIP_TRY(hipGetLastError());
       xd = ws + L.xd;
     }
-    hipLaunchKernelGGL(set_offsets_kernel, dim3(1), dim3(64), 0, st, (int32_t *)(ws + L.offs), T);
-    HIP_TRY(hipGetLastError());
     const GemmProblem p[2] = {problem(T, di, dx, 0, dy, W_T, dn), problem(T, r, V, 1, dy, ws + L.Bt, dn)};
     HIP_TRY(launch_gemm(dt, p, 2, st));
-    if (drop.thr) HIP_TRY(launch_masked_add<float>((float *)dx, V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
-    else HIP_TRY(launch_lowrank_add(dt, dx, V, ws + L.At, T, di, r, s, st));
+    HIP_TRY(launch_masked_add<float>((const float *)dx, V, ws + L.At, dx, T, di, r, drop.thr ? s * drop.inv : s, drop,
+                                     (int32_t *)(ws + L.offs), st));
     const GoJob go[2] = {GoJob{offs, nullptr, V, (const float *)xd, dA, 1, r, di, 1, T, 1, s},
                          GoJob{offs, nullptr, P, (const float *)dy, dB, 1, r, dn, 1, T, 0, s}};
     HIP_TRY(launch_group_outer(go, 2, part, L.partial_floats, st));
@@ -522,7 +528,7 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       p.C = ws + L.dx32;
       p.c_f32 = 1;
       HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
-      HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, st));
+      HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, nullptr, st));
     }
     const GomJob go[2] = {
         GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 0, drop},

@@ -223,13 +223,14 @@ template <int PER> static hipError_t launch_few_m(const Q4Matrix &w, const Q4Few
   return launch_few_n<4, PER, false>(w, a, st);
 }
 
-// ---- everything else up to 128 rows: slices of the contraction, then their sum with the rank-r term --------
+// ---- everything else: slices of the contraction, then their sum with the rank-r term ------------------------
 // A workgroup owns NT tiles' rows and a slice of the contraction.  Its eight wavefronts are WM groups of MT row
-// blocks times 8 / WM shares of the slice.  Trailing workgroups make slices of the projection D(x) A^T.
+// blocks times 8 / WM shares of the slice.  Up to 128 rows trailing workgroups make slices of the projection D(x) A^T; of more
+// rows (which come with their projection) every workgroup takes 128.
 constexpr int Q4S_NT = 4;
 struct Q4Slices {
   int S, per;              // slices, tiles of each
-  int main;                // workgroups of the product
+  int blocks, main;        // 128-row blocks of x; workgroups of the product
   int PS;                  // slices of the projection, of eight tiles: one per wavefront
   float *part, *ppart;     // [S][T][n], [PS][T][r]
 };
@@ -242,9 +243,9 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
   float *red = reinterpret_cast<float *>(smem);
   static_assert(NT >= 4, "the staging fits");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l15 = lane & 15, hi = lane >> 4;
-  const int T = a.T, r = a.r, K = w.K, kbs = (int)q4_col_blocks(K);
+  const int r = a.r, K = w.K, kbs = (int)q4_col_blocks(K);
   if ((int)blockIdx.x >= z.main) {   // a slice of the projection of 16 rows: one tile of the contraction per wavefront
-    const int nq = (r + 15) >> 4, at = blockIdx.x - z.main, ps = at % z.PS, t0 = at / z.PS * 16;
+    const int T = a.T, nq = (r + 15) >> 4, at = blockIdx.x - z.main, ps = at % z.PS, t0 = at / z.PS * 16;
     const int kb = ps * 8 + wave, row = t0 + l15 < T ? t0 + l15 : T - 1;
     unsigned char *stage = smem + wave * STAGE_BYTES;
     f32x4_t p[4];
@@ -291,7 +292,9 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
     }
     return;
   }
-  const int groups = z.main / z.S, rb0 = blockIdx.x % groups * NT, sl = blockIdx.x / groups;
+  const int groups = z.main / (z.S * z.blocks), rb0 = blockIdx.x % groups * NT, at = blockIdx.x / groups;
+  const int tb = at % z.blocks * 128, sl = at / z.blocks, T = a.T - tb;   // rows from tb on, of which this one takes 128
+  const bf16_t *x0 = a.x + (int64_t)tb * K;
   const int row_blocks = (int)q4_row_blocks(w.n);
   const int wm = wave / WK, wk = wave % WK;
   const int lo = sl * z.per, end = lo + z.per < kbs ? lo + z.per : kbs;
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
   for (int kb = lo + wk; kb < end; kb += WK) {
     bf16x8_t fx[MT][4], x[MT][4];
 #pragma unroll
-    for (int m = 0; m < MT; m++) rows_load(a.x, RowOffsets((wm * MT + m) * 16, T, K, lane), kb, K, lane, x[m]);
+    for (int m = 0; m < MT; m++) rows_load(x0, RowOffsets((wm * MT + m) * 16, T, K, lane), kb, K, lane, x[m]);
     wave_order();
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_to_lds(stage + m * STAGE_BYTES, x[m], kb, K, lane);
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
 #pragma unroll
       for (int e = 0; e < 4; e++) v[e] += p[4 * e];
     }
-    *reinterpret_cast<f32x4_t *>(z.part + ((int64_t)sl * T + t) * w.n + n) = v;
+    *reinterpret_cast<f32x4_t *>(z.part + ((int64_t)sl * a.T + tb + t) * w.n + n) = v;
   }
 }
 
@@ -414,14 +417,62 @@ static Q4Slices plan_slices(int n, int K, int T) {
   Q4Slices z{};
   const int kbs = (int)q4_col_blocks(K), groups = (int)((q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT);
   const int wk = T <= 64 ? 8 : 4;
-  int S = 256 / groups;
+  z.blocks = (T + 127) / 128;
+  int S = 256 / (groups * z.blocks);
   const int most = (kbs + wk - 1) / wk;
   S = S > most ? most : S < 1 ? 1 : S > 16 ? 16 : S;
   z.per = (kbs + S - 1) / S;
   z.S = (kbs + z.per - 1) / z.per;
-  z.main = groups * z.S;
+  z.main = groups * z.blocks * z.S;
   z.PS = (kbs + 7) / 8;
   return z;
+}
+
+// More than 128 rows: while the workgroups are not much more than the chip holds at once; beyond, widening the matrix
+// for the large product costs less than reading x per 64 columns (us, here / widened: 129 tokens 4096 -> 4096 29.7 /
+// 39.5, 512 45.6 / 55.2, 700 71.9 / 63.6; 200 4096 -> 11008 65.3 / 84.6, 300 90.4 / 88.6; 517 4096 -> 1024 27.6 /
+// 33.1, 2000 50.5 / 47.1).
+bool q4_mid_ok(int n, int K, int T) {
+  const int64_t groups = (q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT;
+  return T > Q4_FEW_ROWS && T <= 1024 && K < 1 << 23 && groups * ((T + 127) / 128) <= 384;
+}
+size_t q4_mid_scratch_floats(int n, int K, int T) { return (size_t)plan_slices(n, K, T).S * T * n; }
+
+#define MIXLORA_SLICES(MT_, WM_, PER_)                                                                                   \
+  do {                                                                                                                   \
+    constexpr size_t lds_ = (size_t)8 * Q4S_NT * MT_ * 1024;                                                              \
+    static const hipError_t e_ = hipFuncSetAttribute((const void *)q4_slices_kernel<MT_, WM_, PER_>,                     \
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_);             \
+    if (e_ != hipSuccess) return e_;                                                                                     \
+    hipLaunchKernelGGL((q4_slices_kernel<MT_, WM_, PER_>), grid, block, lds_, st, w, a, z, drop);                        \
+  } while (0)
+#define MIXLORA_BY_GROUP(LAUNCH)        \
+  do {                                  \
+    if (w.group == 128) LAUNCH(1);      \
+    else if (w.group == 64) LAUNCH(2);  \
+    else LAUNCH(4);                     \
+  } while (0)
+#define MIXLORA_S1(PER_) MIXLORA_SLICES(1, 1, PER_)
+#define MIXLORA_S2(PER_) MIXLORA_SLICES(2, 1, PER_)
+#define MIXLORA_S4(PER_) MIXLORA_SLICES(4, 1, PER_)
+#define MIXLORA_S8(PER_) MIXLORA_SLICES(4, 2, PER_)
+
+hipError_t launch_q4_mid(const Q4Matrix &w, const Q4Few &a, const float *P, float *scratch, size_t floats, hipStream_t st) {
+  Q4Slices z = plan_slices(w.n, w.K, a.T);
+  if (!q4_mid_ok(w.n, w.K, a.T) || a.r % 8 || a.r > 64 || w.n % 8 || w.K % 8 || (size_t)z.S * a.T * w.n > floats)
+    return hipErrorInvalidValue;
+  const int slot = prof_on() ? prof_mark_begin(PROF_GEMM, st) : -1;
+  z.part = scratch;
+  z.ppart = const_cast<float *>(P);   // one slice, read only
+  z.PS = 1;
+  const DropArgs drop{};
+  const dim3 grid(z.main), block(512);
+  MIXLORA_BY_GROUP(MIXLORA_S8);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(q4_finish_kernel, dim3((w.n + 63) / 64, (a.T + 15) / 16), dim3(256), 0, st, w.n, a, z);
+  if (slot >= 0) prof_mark_end(slot, st, 2.0 * a.T * w.n * w.K);
+  return hipGetLastError();
 }
 
 size_t q4_few_scratch_floats(int n, int K, int T, int r) {
@@ -433,12 +484,6 @@ size_t q4_few_scratch_floats(int n, int K, int T, int r) {
 hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop, float *scratch, size_t floats, hipStream_t st) {
   if (a.T < 1 || a.T > Q4_FEW_ROWS || a.r % 8 || a.r > 64 || w.K >= 1 << 23 || w.n % 8 || w.K % 8) return hipErrorInvalidValue;
   const int slot = prof_on() ? prof_mark_begin(PROF_GEMM, st) : -1;
-#define MIXLORA_BY_GROUP(LAUNCH)        \
-  do {                                  \
-    if (w.group == 128) LAUNCH(1);      \
-    else if (w.group == 64) LAUNCH(2);  \
-    else LAUNCH(4);                     \
-  } while (0)
   if (one_launch(a.T, w.K, a.r, drop.thr != 0)) {
     const hipError_t e = w.group == 128 ? launch_few_m<1>(w, a, st) : w.group == 64 ? launch_few_m<2>(w, a, st) : launch_few_m<4>(w, a, st);
     if (e != hipSuccess) return e;
@@ -448,18 +493,6 @@ hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop
     z.part = scratch;
     z.ppart = scratch + (size_t)z.S * a.T * w.n;
     const dim3 grid(z.main + (a.T + 15) / 16 * z.PS), block(512);
-#define MIXLORA_SLICES(MT_, WM_, PER_)                                                                                   \
-  do {                                                                                                                   \
-    constexpr size_t lds_ = (size_t)8 * Q4S_NT * MT_ * 1024;                                                              \
-    static const hipError_t e_ = hipFuncSetAttribute((const void *)q4_slices_kernel<MT_, WM_, PER_>,                     \
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_);             \
-    if (e_ != hipSuccess) return e_;                                                                                     \
-    hipLaunchKernelGGL((q4_slices_kernel<MT_, WM_, PER_>), grid, block, lds_, st, w, a, z, drop);                        \
-  } while (0)
-#define MIXLORA_S1(PER_) MIXLORA_SLICES(1, 1, PER_)
-#define MIXLORA_S2(PER_) MIXLORA_SLICES(2, 1, PER_)
-#define MIXLORA_S4(PER_) MIXLORA_SLICES(4, 1, PER_)
-#define MIXLORA_S8(PER_) MIXLORA_SLICES(4, 2, PER_)
     if (a.T <= 16) MIXLORA_BY_GROUP(MIXLORA_S1);
     else if (a.T <= 32) MIXLORA_BY_GROUP(MIXLORA_S2);
     else if (a.T <= 64) MIXLORA_BY_GROUP(MIXLORA_S4);

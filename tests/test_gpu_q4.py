@@ -152,6 +152,14 @@ CASES = [
     (200, 512, 1032, 16, 64, "bf16", 0.0),
     (257, 136, 520, 64, 128, "bf16", 0.05),
     (300, 776, 264, 8, 32, "bf16", 0.0),
+    (1024, 264, 72, 16, 64, "bf16", 0.05),
+    (1025, 264, 72, 16, 64, "bf16", 0.05),
+    (1100, 136, 520, 8, 32, "bf16", 0.0),
+    (130, 264, 12304, 8, 64, "bf16", 0.0),
+    (257, 264, 8208, 8, 64, "bf16", 0.0),
+    (40, 8456, 72, 16, 64, "bf16", 0.0),
+    (33, 264, 4120, 16, 32, "bf16", 0.0),
+    (9, 264, 8216, 16, 64, "bf16", 0.0),
     (1, 136, 24, 8, 64, "f32", 0.0),
     (7, 72, 40, 12, 32, "f32", 0.2),
     (97, 136, 264, 16, 128, "f32", 0.0),
@@ -242,7 +250,7 @@ def test_forward_alone_in_its_workspace(T):
     assert np.array_equal(m.y.numpy(), first)
 
 
-@pytest.mark.parametrize("T", [1, 9, 40, 128, 150])
+@pytest.mark.parametrize("T", [1, 9, 40, 128, 150, 1030])
 def test_codes_of_every_kind_are_exact(T):
     """Whole numbers: every code, scales 1, 2, 4, x of small integers; sums below 2^24 are exact in fp32, and
     results of at most eight bits in bf16.  One row of x picks one input, so every place of every tile shows."""
@@ -265,7 +273,7 @@ def test_codes_of_every_kind_are_exact(T):
     assert not got["dA"].any() and not got["dB"].any()
 
 
-@pytest.mark.parametrize("T", [2, 30, 150])
+@pytest.mark.parametrize("T", [2, 30, 150, 1030])
 def test_groups_that_are_not_numbers(T):
     """A NaN scale makes its row of W' NaN and no other; infinite inputs spread as in 64 bits."""
     h, W = problem(T, 264, 40, 8, 64, "bf16", 11)
@@ -288,7 +296,7 @@ def test_groups_that_are_not_numbers(T):
     assert np.array_equal(np.isfinite(y), np.isfinite(want))
 
 
-@pytest.mark.parametrize("T", [3, 70, 150])
+@pytest.mark.parametrize("T", [3, 70, 150, 1030])
 def test_scales_of_eight_bits(T):
     """Scales that a checkpoint brings: scale x level has up to ten significant bits and may be rounded to bf16
     before it is multiplied, which is half a step (2^-8) of every product more, |x| |W'|^T in all."""

@@ -60,6 +60,34 @@ def test_quantize_is_idempotent_and_near():
         assert np.array_equal(orc.values(c2, s2, group), V)
 
 
+def test_arrays_against_single_elements():
+    """The oracle's array forms against its definitions of one code, one byte and one counter."""
+    rng = np.random.default_rng(4)
+    W = rng.normal(0, 1, (20, 200))
+    W[3, :40] = [0.0, -0.0] * 20
+    W[5, 150], W[6, 10] = np.nan, np.inf
+    W[7, :32] = np.resize(np.array([9.0, .375, 1.125, 1.875, 2.625, 3.75, 5.25, -7.5]), 32)
+    for group in (32, 64, 128):
+        codes, scales = orc.quantize(W, group)
+        data, sc = orc.pack(codes, scales, group)
+        kt, per = 2, 128 // group
+        for i in range(20):
+            for k in range(200):
+                g = k // group
+                assert codes[i, k] == orc.nearest_code(W[i, k], scales[i, g]), (i, k)
+                byte = data[(i // 16 * kt + k // 128) * 1024 + 16 * (16 * (k % 32 // 8) + i % 16) + 4 * (k % 128 // 32) + k % 8 // 2]
+                assert (byte >> (4 * (k % 2))) & 15 == codes[i, k]
+                got = sc[((i // 16 * kt + g // per) * 16 + i % 16) * per + g % per]
+                assert got == scales[i, g] or np.isnan(got) and np.isnan(scales[i, g])
+        assert data.size == 4 * 1024 and sc.size == 4 * 16 * per
+    f = orc.dropout_factors(3, 20, 0.3, 0x123456789ABCDEF0, (9 << 32) + 4)
+    thr = int(np.floor(float(np.float32(0.3)) * 65536 + 0.5))
+    for t in range(3):
+        for c in range(20):
+            w = orc.philox((c // 8, t, 4, 9), (0x9ABCDEF0, 0x12345678))[c % 8 // 2] >> (16 * (c % 2)) & 0xFFFF
+            assert f[t, c] == (65536 / (65536 - thr) if w >= thr else 0.0)
+
+
 def test_linear_against_autograd():
     rng = np.random.default_rng(2)
     x, W, A, B, dy = (rng.normal(size=n) for n in ((9, 16), (24, 16), (3, 16), (24, 3), (9, 24)))
@@ -91,7 +119,7 @@ def test_router_against_autograd_and_differences(mode):
     zl = 0.2 * torch.logsumexp(t[on], 1).square().mean()
     w = p[on].gather(1, idx[on])
     w = w / w.sum(1, keepdim=True)
-    assert np.allclose(got["loss"], [float(bal + zl), float(bal), float(zl)], rtol=1e-12)
+    assert np.allclose(got["loss"], [(bal + zl).item(), bal.item(), zl.item()], rtol=1e-12)
     assert np.allclose(got["topk_w"][mask], w.detach().numpy(), rtol=1e-12)
     (0.7 * bal + 1.3 * zl + (w * torch.tensor(dw)[on]).sum()).backward()
     assert np.allclose(got["dlogits"], t.grad.numpy(), rtol=1e-10, atol=1e-14)
