@@ -244,14 +244,15 @@ __global__ __launch_bounds__(RL_THREADS) void router_loss_backward_kernel(Router
     }
     const float cb = gb * a.balance * (float)N * inv, cz = gz * a.zc * 2.f * inv * lse;
     // w = p over the kept ones' sum;  dz = w (dw - sum_j w_j dw_j) + the losses' share
-    const float rs = kept ? 1.f / sum : 0.f;
+    // (divided, not multiplied with a reciprocal: the weight of a single kept expert is 1 and its gradient nothing, beside
+    // which the losses' share is small)
     float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < NR; i++) dot = kept >> i & 1 ? fmaf(z[i] * rs, g[i], dot) : dot;
+    for (int i = 0; i < NR; i++) dot = kept >> i & 1 ? fmaf(z[i] / sum, g[i], dot) : dot;
 #pragma unroll
     for (int i = 0; i < NR; i++) {
       const float l = i < N ? z[i] * (cb * (a.stats[i] - fp) + cz) : 0.f;
-      g[i] = kept >> i & 1 ? fmaf(z[i] * rs, g[i] - dot, l) : l;
+      g[i] = kept >> i & 1 ? fmaf(z[i] / sum, g[i] - dot, l) : l;
     }
   }
   E *out = (E *)dz + t * N;

@@ -121,6 +121,18 @@ def test_ties_and_extremes():
     assert np.isnan(got["dlogits"][4]).all() and np.array_equal(got["topk_idx"][:4], [[0, 1], [1, 3], [1, 0], [0, 3]])
 
 
+@pytest.mark.parametrize("T,N,dtype", [(300, 8, "f32"), (77, 5, "f32"), (129, 64, "bf16"), (2000, 16, "f32")])
+def test_one_kept_expert_passes_no_gradient(T, N, dtype):
+    """k = 1: the weight is 1 whatever the logits are, so d_topk_w, however large beside the losses, changes nothing."""
+    rng = np.random.default_rng(T)
+    z = rounded(rng.normal(0, 1.5, (T, N)), dtype)
+    mask = rng.random(T) < 0.7
+    dw = (1e3 * rng.normal(size=(T, 1))).astype(np.float32)
+    with_dw, without = run(z, mask, 1, "top1", dtype, dw), run(z, mask, 1, "top1", dtype, None)
+    assert np.all(with_dw["topk_w"][mask] == 1)
+    assert np.array_equal(with_dw["dlogits"], without["dlogits"]) and without["dlogits"].any()
+
+
 def test_reruns_and_graph():
     rng = np.random.default_rng(9)
     T, N, k = 3000, 16, 2
