@@ -223,6 +223,50 @@ template <int PER> static hipError_t launch_few_m(const Q4Matrix &w, const Q4Few
   return launch_few_n<4, PER, false>(w, a, st);
 }
 
+// The same with the codes as the first operand: a lane has four neighbouring columns of y of one row instead of four rows of a
+// column, which is how sums are then added and written 16 bytes at a time.  It takes the scales of its four columns,
+// [column][group] as they are held.
+template <int PER> struct Q4Scales4 { uint32_t w[2 * PER]; };
+template <int PER>
+__device__ __forceinline__ void q4_load4(const Q4Matrix &w, int64_t tile, int lane, uint4 &c, Q4Scales4<PER> &s) {
+  c = *reinterpret_cast<const uint4 *>(w.codes + tile * Q4_TILE_BYTES + (uint32_t)lane * 16u);
+  const bf16_t *p = w.scales + tile * (Q4_ROWS * PER) + (uint32_t)(lane >> 4) * (4 * PER);
+  if constexpr (PER == 1) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    s.w[0] = v.x, s.w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER / 2; i++) {
+      const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+      s.w[4 * i] = v.x, s.w[4 * i + 1] = v.y, s.w[4 * i + 2] = v.z, s.w[4 * i + 3] = v.w;
+    }
+  }
+}
+template <int MT, int PER>
+__device__ __forceinline__ void q4_tile4(const bf16x8_t (&fx)[MT][4], const uint4 &c, const Q4Scales4<PER> &s, f32x4_t (&acc)[MT]) {
+  const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+  constexpr int STEPS = 4 / PER;
+#pragma unroll
+  for (int g = 0; g < PER; g++) {
+    f32x4_t part[MT];
+#pragma unroll
+    for (int m = 0; m < MT; m++) part[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = g * STEPS; st < (g + 1) * STEPS; st++) {
+      const bf16x8_t fw = q4_operand(word[st]);
+#pragma unroll
+      for (int m = 0; m < MT; m++) part[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw, fx[m][st], part[m], 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+      const int at = u * PER + g;
+      const float sc = __uint_as_float(at & 1 ? s.w[at >> 1] & 0xffff0000u : s.w[at >> 1] << 16);
+#pragma unroll
+      for (int m = 0; m < MT; m++) acc[m][u] = fmaf(sc, part[m][u], acc[m][u]);
+    }
+  }
+}
+
 // ---- everything else: slices of the contraction, then their sum with the rank-r term ------------------------
 // A workgroup owns NT tiles' rows and a slice of the contraction.  Its eight wavefronts are WM groups of MT row
 // blocks times 8 / WM shares of the slice.  Up to 128 rows trailing workgroups make slices of the projection D(x) A^T; of more
@@ -308,12 +352,10 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
     for (int m = 0; m < MT; m++) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   unsigned char *stage = smem + wave * MT * STAGE_BYTES;
   uint4 nc[NT];
-  float ns[NT][PER];
+  Q4Scales4<PER> ns[NT];
   auto load_w = [&](int kb) {
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-      q4_load<PER>(w, first[i] + kb, lane, nc[i], ns[i]);
-    }
+    for (int i = 0; i < NT; i++) q4_load4<PER>(w, first[i] + kb, lane, nc[i], ns[i]);
   };
   if (lo + wk < end) load_w(lo + wk);
   for (int kb = lo + wk; kb < end; kb += WK) {
@@ -324,19 +366,15 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_to_lds(stage + m * STAGE_BYTES, x[m], kb, K, lane);
     uint4 c[NT];
-    float s[NT][PER];
+    Q4Scales4<PER> s[NT];
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-      c[i] = nc[i];
-#pragma unroll
-      for (int g = 0; g < PER; g++) s[i][g] = ns[i][g];
-    }
+    for (int i = 0; i < NT; i++) c[i] = nc[i], s[i] = ns[i];
     wave_order();
     if (kb + WK < end) load_w(kb + WK);
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_from_lds(stage + m * STAGE_BYTES, lane, fx[m]);
 #pragma unroll
-    for (int i = 0; i < NT; i++) q4_tile<MT, PER>(fx, c[i], s[i], acc[i]);
+    for (int i = 0; i < NT; i++) q4_tile4<MT, PER>(fx, c[i], s[i], acc[i]);
   }
   __syncthreads();   // the staging is behind everybody
 #pragma unroll
@@ -344,19 +382,14 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
 #pragma unroll
     for (int m = 0; m < MT; m++) *reinterpret_cast<f32x4_t *>(red + (((wave * NT + i) * MT + m) * 64 + lane) * 4) = acc[i][m];
   __syncthreads();
-  // four columns of a token per thread: 16 threads write 64 columns of it
-  for (int o = tid; o < WM * MT * 16 * (NT * 4); o += 512) {
-    const int c4 = o % (NT * 4), t = o / (NT * 4), i = c4 >> 2, c0 = (c4 & 3) * 4;
-    const int n = (rb0 + i) * 16 + c0;
+  // lane (l15, hi), register u: row l15, column 4 hi + u
+  for (int o = tid; o < WM * NT * MT * 64; o += 512) {
+    const int ln = o & 63, m = (o >> 6) % MT, i = (o >> 6) / MT % NT, g = (o >> 6) / (MT * NT);
+    const int t = (g * MT + m) * 16 + (ln & 15), n = (rb0 + i) * 16 + (ln >> 4) * 4;
     if (t >= T || n >= w.n) continue;
-    const int g = t / (16 * MT), m = t / 16 % MT, tl = t & 15;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < WK; k++) {
-      const float *p = red + ((((g * WK + k) * NT + i) * MT + m) * 64 + (tl >> 2) * 16 + c0) * 4 + (tl & 3);
-#pragma unroll
-      for (int e = 0; e < 4; e++) v[e] += p[4 * e];
-    }
+    for (int k = 0; k < WK; k++) v += *reinterpret_cast<const f32x4_t *>(red + ((((g * WK + k) * NT + i) * MT + m) * 64 + ln) * 4);
     *reinterpret_cast<f32x4_t *>(z.part + ((int64_t)sl * a.T + tb + t) * w.n + n) = v;
   }
 }
@@ -418,13 +451,13 @@ static Q4Slices plan_slices(int n, int K, int T) {
   const int kbs = (int)q4_col_blocks(K), groups = (int)((q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT);
   const int wk = T <= 64 ? 8 : 4;
   z.blocks = (T + 127) / 128;
+  z.PS = (kbs + 7) / 8;
   int S = 256 / (groups * z.blocks);
   const int most = (kbs + wk - 1) / wk;
   S = S > most ? most : S < 1 ? 1 : S > 16 ? 16 : S;
   z.per = (kbs + S - 1) / S;
   z.S = (kbs + z.per - 1) / z.per;
   z.main = groups * z.blocks * z.S;
-  z.PS = (kbs + 7) / 8;
   return z;
 }
 
