@@ -8,6 +8,8 @@
 #include "dropout.h"
 #include "rows_stage.h"
 
+#include <type_traits>
+
 namespace mixlora {
 
 typedef bf16_t bf16x2_t __attribute__((ext_vector_type(2)));
@@ -228,8 +230,7 @@ template <int PER> static hipError_t launch_few_m(const Q4Matrix &w, const Q4Few
 // [column][group] as they are held.
 template <int PER> struct Q4Scales4 { uint32_t w[2 * PER]; };
 template <int PER>
-__device__ __forceinline__ void q4_load4(const Q4Matrix &w, int64_t tile, int lane, uint4 &c, Q4Scales4<PER> &s) {
-  c = *reinterpret_cast<const uint4 *>(w.codes + tile * Q4_TILE_BYTES + (uint32_t)lane * 16u);
+__device__ __forceinline__ void q4_load_scales4(const Q4Matrix &w, int64_t tile, int lane, Q4Scales4<PER> &s) {
   const bf16_t *p = w.scales + tile * (Q4_ROWS * PER) + (uint32_t)(lane >> 4) * (4 * PER);
   if constexpr (PER == 1) {
     const uint2 v = *reinterpret_cast<const uint2 *>(p);
@@ -264,6 +265,30 @@ __device__ __forceinline__ void q4_tile4(const bf16x8_t (&fx)[MT][4], const uint
 #pragma unroll
       for (int m = 0; m < MT; m++) acc[m][u] = fmaf(sc, part[m][u], acc[m][u]);
     }
+  }
+}
+
+// In groups of 32 and with four row blocks the scales of four columns, a product per group and block, cost more than scaling
+// the operand: scale x level goes into bf16, exactly for scales of six significant bits (517 tokens 4096 -> 1024 28.8 ->
+// 25.8 us).  A lane takes the four scales of one row.
+template <int MT>
+__device__ __forceinline__ void q4_tile_scaled(const bf16x8_t (&fx)[MT][4], const uint4 &c, const uint2 &sc, f32x4_t (&acc)[MT]) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int st = 0; st < 4; st++) {
+    const uint32_t h = st < 2 ? sc.x : sc.y;
+    const float s = __uint_as_float(st & 1 ? h & 0xffff0000u : h << 16);
+    f32x2_t p[4];
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[st], 1.f, 0);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[st], 1.f, 1);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[st], 1.f, 2);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[st], 1.f, 3);
+    bf16x8_t fw;
+#pragma unroll
+    for (int e = 0; e < 8; e++) fw[e] = (bf16_t)(s * p[e >> 1][e & 1]);
+#pragma unroll
+    for (int m = 0; m < MT; m++) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw, fx[m][st], acc[m], 0, 0, 0);
   }
 }
 
@@ -351,30 +376,41 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
 #pragma unroll
     for (int m = 0; m < MT; m++) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   unsigned char *stage = smem + wave * MT * STAGE_BYTES;
-  uint4 nc[NT];
-  Q4Scales4<PER> ns[NT];
+  uint4 nc[NT];   // codes come one tile ahead; scales with them would not fit the registers in groups of 32
   auto load_w = [&](int kb) {
 #pragma unroll
-    for (int i = 0; i < NT; i++) q4_load4<PER>(w, first[i] + kb, lane, nc[i], ns[i]);
+    for (int i = 0; i < NT; i++)
+      nc[i] = *reinterpret_cast<const uint4 *>(w.codes + (first[i] + kb) * Q4_TILE_BYTES + (uint32_t)lane * 16u);
   };
   if (lo + wk < end) load_w(lo + wk);
   for (int kb = lo + wk; kb < end; kb += WK) {
     bf16x8_t fx[MT][4], x[MT][4];
+    constexpr bool SCALED = PER == 4 && MT == 4;
+    typename std::conditional<SCALED, uint2, Q4Scales4<PER>>::type s[NT];
+#pragma unroll
+    for (int i = 0; i < NT; i++) {
+      if constexpr (SCALED)
+        s[i] = *reinterpret_cast<const uint2 *>(w.scales + (first[i] + kb) * (Q4_ROWS * 4) + (uint32_t)l15 * 4);
+      else
+        q4_load_scales4<PER>(w, first[i] + kb, lane, s[i]);
+    }
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_load(x0, RowOffsets((wm * MT + m) * 16, T, K, lane), kb, K, lane, x[m]);
     wave_order();
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_to_lds(stage + m * STAGE_BYTES, x[m], kb, K, lane);
     uint4 c[NT];
-    Q4Scales4<PER> s[NT];
 #pragma unroll
-    for (int i = 0; i < NT; i++) c[i] = nc[i], s[i] = ns[i];
+    for (int i = 0; i < NT; i++) c[i] = nc[i];
     wave_order();
     if (kb + WK < end) load_w(kb + WK);
 #pragma unroll
     for (int m = 0; m < MT; m++) rows_from_lds(stage + m * STAGE_BYTES, lane, fx[m]);
 #pragma unroll
-    for (int i = 0; i < NT; i++) q4_tile4<MT, PER>(fx, c[i], s[i], acc[i]);
+    for (int i = 0; i < NT; i++) {
+      if constexpr (SCALED) q4_tile_scaled<MT>(fx, c[i], s[i], acc[i]);
+      else q4_tile4<MT, PER>(fx, c[i], s[i], acc[i]);
+    }
   }
   __syncthreads();   // the staging is behind everybody
 #pragma unroll
