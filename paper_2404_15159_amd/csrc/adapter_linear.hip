@@ -1,11 +1,11 @@
 // LoRA linear with dropout on the adapter's input, on an ordinary or on a 4-bit frozen matrix:
 //   y = x W^T + s (D(x) A^T) B^T,   dx = dy W + D'(s (dy B) A),   dA = s (dy B)^T D(x),   dB = s dy^T (D(x) A^T)
-// D drops elements and scales the others (dropout.h makes the mask from counters wherever it is needed),
-// D' drops the same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen
-// product as an extra K segment, in three bf16 pieces that hold all of its 24 bits; the backward's, which has to
-// be masked with dropout, goes first and is masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as
-// well.  A 4-bit matrix is widened into the workspace, which rounds nothing (q4.h), but for the forward of few rows,
-// which multiplies with the codes (q4_few.hip).
+// D drops elements and scales the others (dropout.h makes the mask from counters wherever it is needed), D' drops the
+// same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen product as an extra K segment,
+// in three bf16 pieces that hold all of its 24 bits; the backward's, which has to be masked with dropout, goes first and is
+// masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as well.  A 4-bit matrix is widened
+// into the workspace, which rounds nothing (q4.h), but for the forward of few rows, which multiplies with the codes
+// (q4_few.hip).  fp32: D(x) is made in the workspace, and the products are the fp32 ones.
 #include "common.h"
 #include "q4.h"
 #include "q4_few.h"
@@ -101,7 +101,7 @@ int check_q4(const mixlora_linear_dims &D, const mixlora_q4 *q4) {
   return misaligned(q4->codes) || misaligned(q4->scales) ? MIXLORA_E_ALIGN : MIXLORA_OK;
 }
 
-// p in [0, 1) to sixteenths of a bit of its 16 bits; all of 1 - 2^-17 and above would drop everything
+// p in [0, 1), held in 16 bits; from 1 - 2^-17 on it would drop everything
 int make_drop(const mixlora_dropout *d, DropArgs &out) {
   out = DropArgs{};
   if (!d) return MIXLORA_OK;

@@ -1,8 +1,9 @@
-// Products of few rows (up to 128) with a 4-bit frozen matrix, and the rank-r term of a LoRA linear on it:
+// Products of few rows (up to 1024) with a 4-bit frozen matrix, and the rank-r term of a LoRA linear on it:
 //   y = x W'^T + s (D(x) A^T) B^T.
-// Bound by reading the codes once.  Codes go from memory to registers as a wavefront's MFMA operand (q4.h) and
-// are widened there, two per instruction; levels are exact in bf16, so x times level is summed in fp32 as it is
-// and a group's sum is multiplied by the group's scale in fp32: nothing is rounded before y.
+// Bound by reading the codes once, and from some tens of rows on by reading x for every 64 columns.  Codes go from memory
+// to registers as a wavefront's MFMA operand (q4.h) and are widened there, two per instruction; levels are exact in bf16,
+// so x times level is summed in fp32 as it is and a group's sum is multiplied by the group's scale in fp32: nothing is
+// rounded before y (but see q4_tile_scaled).
 #include "q4.h"
 #include "q4_few.h"
 #include "dropout.h"
