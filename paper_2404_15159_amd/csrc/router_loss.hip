@@ -18,7 +18,7 @@ using namespace mixlora;
 namespace {
 
 constexpr int RL_THREADS = 64;   // one wavefront: 16384 tokens are one workgroup per CU
-constexpr int RL_ALL = 1024;     // tokens that one workgroup takes, where a row fits the registers that leaves (N <= 16)
+constexpr int RL_ALL = 1024;     // tokens that one workgroup takes
 struct RouterArgs {
   const void *logits;
   const unsigned char *mask;
@@ -26,7 +26,7 @@ struct RouterArgs {
   float balance, zc;
   int32_t *idx;
   float *w;
-  float *part;          // [wavefront][3 N + 2]: P sums, counts of all slots, of slot 0 (whole numbers), z sum, tokens
+  float *part;          // [workgroup or wavefront][3 N + 2]: P sums, counts of all slots, of slot 0 (whole numbers), z sum, tokens
   float *stats;         // [N + 1]: F, then 1 / n (0 where no token is kept)
   float *loss;
   int32_t *counts;
@@ -271,6 +271,133 @@ __global__ __launch_bounds__(RL_THREADS) void router_loss_backward_kernel(Router
   }
 }
 
+// ---- more than 16 experts: a lane takes an expert, a wavefront four tokens in turn ---------------------------------
+// (with a token per thread, rows of 33 and 64 took 21 and 13 us per direction at 16384 tokens: exponentials and selections of
+// one row behind one another, one wavefront per SIMD)
+// 16 wavefronts per workgroup, four where that leaves most of the chip idle (more partial sums, but of few tokens)
+constexpr int RW_TOKENS = 4, RW_WAVES = 16;
+inline int wide_waves(int T) { return T <= 4096 ? 4 : RW_WAVES; }
+
+template <int CTRL> __device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)));
+}
+__device__ __forceinline__ float lane_value(float v, int l) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
+}
+__device__ __forceinline__ float wave_max(float v) {   // (NaN counts as nothing)
+  v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4e>(dpp_max<0xb1>(v))));
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+// softmax of a row held one element per lane (-inf past N)
+__device__ __forceinline__ float wave_softmax(float z, bool in, float &lse) {
+  const float top = wave_max(z);
+  const float e = in ? expf(z - top) : 0.f;
+  const float sum = wave_total(e);
+  lse = top + logf(sum);
+  return e * (1.f / sum);
+}
+
+template <typename E>
+__global__ __launch_bounds__(RW_WAVES * 64) void router_loss_forward_wide_kernel(RouterArgs a) {
+  __shared__ float sums[RW_WAVES][3][64];
+  __shared__ float zn[RW_WAVES][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = a.N, k = a.k;
+  const int waves = blockDim.x >> 6;
+  const int64_t t0 = ((int64_t)blockIdx.x * waves + wave) * RW_TOKENS;
+  const bool in = lane < N;
+  float zr[RW_TOKENS];
+  bool on[RW_TOKENS];
+#pragma unroll
+  for (int i = 0; i < RW_TOKENS; i++) {   // (a token past the last one: the last one's row, not used)
+    const int64_t t = t0 + i < a.T ? t0 + i : a.T - 1;
+    on[i] = t0 + i < a.T && (!a.mask || a.mask[t]);
+    zr[i] = in ? to_f32(((const E *)a.logits)[t * N + lane]) : -INFINITY;
+  }
+  float P = 0.f, all = 0.f, slot0 = 0.f, zs = 0.f, n = 0.f;
+#pragma unroll
+  for (int i = 0; i < RW_TOKENS; i++) {
+    const int64_t t = t0 + i;
+    if (t >= a.T) break;
+    if (!on[i]) {
+      if (lane < k) a.idx[t * k + lane] = -1, a.w[t * k + lane] = 0.f;
+      continue;
+    }
+    const float raw = isnan(zr[i]) ? -INFINITY : zr[i];   // NaN ranks with -inf
+    float lse;
+    const float p = wave_softmax(zr[i], in, lse);
+    bool left = in;
+    float kept = 0.f, w = 0.f;
+    int e = 0;
+    for (int j = 0; j < k; j++) {   // the largest that is left, the lowest index among equals
+      const float top = wave_max(left ? raw : -INFINITY);
+      const int best = __ffsll((unsigned long long)__ballot(left && raw == top)) - 1;
+      const float pb = lane_value(p, best);
+      kept += pb;
+      if (lane == j) e = best, w = pb;
+      if (lane == best) left = false;
+      if (j == 0 && lane == best) slot0 += 1.f;
+    }
+    if (lane < k) a.idx[t * k + lane] = e, a.w[t * k + lane] = w / kept;
+    P += p;
+    all += in && !left ? 1.f : 0.f;
+    zs += lse * lse;
+    n += 1.f;
+  }
+  sums[wave][0][lane] = P, sums[wave][1][lane] = all, sums[wave][2][lane] = slot0;
+  if (lane == 0) zn[wave][0] = zs, zn[wave][1] = n;
+  __syncthreads();
+  float *out = a.part + (int64_t)blockIdx.x * (3 * N + 2);
+  for (int i = threadIdx.x; i < 3 * N + 2; i += blockDim.x) {
+    float s = 0.f;
+    for (int u = 0; u < waves; u++) s += i < 3 * N ? sums[u][i / N][i % N] : zn[u][i - 3 * N];
+    out[i] = s;
+  }
+}
+
+template <typename E>
+__global__ __launch_bounds__(RW_WAVES * 64) void router_loss_backward_wide_kernel(RouterArgs a, const int32_t *__restrict__ idx,
+                                                                                  const float *__restrict__ dw, float gb, float gz,
+                                                                                  void *__restrict__ dz) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = a.N, k = a.k;
+  const int64_t t0 = ((int64_t)blockIdx.x * (blockDim.x >> 6) + wave) * RW_TOKENS;
+  const bool in = lane < N;
+  const float F = in ? a.stats[lane] : 0.f, inv = a.stats[N];
+  float zr[RW_TOKENS], dr[RW_TOKENS];
+  int er[RW_TOKENS];
+  bool on[RW_TOKENS];
+#pragma unroll
+  for (int i = 0; i < RW_TOKENS; i++) {
+    const int64_t t = t0 + i < a.T ? t0 + i : a.T - 1;
+    on[i] = t0 + i < a.T && (!a.mask || a.mask[t]);
+    zr[i] = in ? to_f32(((const E *)a.logits)[t * N + lane]) : -INFINITY;
+    er[i] = dw && lane < k ? idx[t * k + lane] : -1;
+    dr[i] = dw && lane < k ? dw[t * k + lane] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < RW_TOKENS; i++) {
+    const int64_t t = t0 + i;
+    if (t >= a.T) break;
+    float g = 0.f;
+    if (on[i]) {
+      float lse;
+      const float p = wave_softmax(zr[i], in, lse);
+      bool kept = false;
+      if (dw)
+        for (int j = 0; j < k; j++) {   // the gradient of a kept expert's weight to its lane
+          const int e = __builtin_amdgcn_readlane(er[i], j);
+          if (lane == e) kept = true, g = lane_value(dr[i], j);
+        }
+      kept = kept && in;
+      const float fp = wave_total(F * p), sum = wave_total(kept ? p : 0.f);
+      const float w = kept ? p / sum : 0.f;   // (divided: the weight of a single kept expert is 1)
+      const float dot = wave_total(kept ? w * g : 0.f);
+      const float l = p * (gb * a.balance * (float)N * inv * (F - fp) + gz * a.zc * 2.f * inv * lse);
+      g = kept ? fmaf(w, g - dot, l) : l;
+    }
+    if (in) ((E *)dz)[t * N + lane] = from_f32<E>(g);
+  }
+}
+
 int check(const mixlora_router_dims *D) {
   if (!D) return MIXLORA_E_NULL;
   if (D->dtype != MIXLORA_F32 && D->dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
@@ -281,6 +408,7 @@ int check(const mixlora_router_dims *D) {
 }
 inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 inline int blocks_of(int T) { return (T + RL_THREADS - 1) / RL_THREADS; }
+inline int wide_blocks(int T) { return (T + wide_waves(T) * RW_TOKENS - 1) / (wide_waves(T) * RW_TOKENS); }
 inline size_t stats_bytes(int N) { return ((size_t)(N + 1) * 4 + 255) / 256 * 256; }
 
 RouterArgs args_of(const mixlora_router_dims &D, const void *logits, const unsigned char *mask, void *ws) {
@@ -295,12 +423,9 @@ RouterArgs args_of(const mixlora_router_dims &D, const void *logits, const unsig
 template <typename E, int NR, bool FULL>
 hipError_t launch_forward(const RouterArgs &a, hipStream_t st) {
   const int waves = blocks_of(a.T);
-  if constexpr (NR <= 16) {
-    if (a.T <= RL_ALL) {   // (300 x 8: 2.7 us of a second launch)
-      const int threads = waves * 64 < 64 ? 64 : waves * 64;
-      hipLaunchKernelGGL((router_loss_forward_kernel<E, NR, FULL, true>), dim3(1), dim3(threads), 0, st, a);
-      return hipGetLastError();
-    }
+  if (a.T <= RL_ALL) {   // (300 x 8: 2.7 us of a second launch)
+    hipLaunchKernelGGL((router_loss_forward_kernel<E, NR, FULL, true>), dim3(1), dim3(waves * 64), 0, st, a);
+    return hipGetLastError();
   }
   hipLaunchKernelGGL((router_loss_forward_kernel<E, NR, FULL, false>), dim3(waves), dim3(RL_THREADS), 0, st, a);
   const hipError_t e = hipGetLastError();
@@ -313,15 +438,26 @@ hipError_t launch_backward(const RouterArgs &a, const int32_t *idx, const float 
   hipLaunchKernelGGL((router_loss_backward_kernel<E, NR, FULL>), dim3(blocks_of(a.T)), dim3(RL_THREADS), 0, st, a, idx, dw, gb, gz, dz);
   return hipGetLastError();
 }
-// one instance per storage type and row length, with whole rows of 8, 16 and 64 apart
+// one instance per storage type and row length up to 16, with whole rows of 8 and 16 apart
 template <typename F>
 hipError_t by_row(int N, F &&f) {
   if (N == 8) return f(std::integral_constant<int, 8>{}, std::true_type{});
   if (N < 8) return f(std::integral_constant<int, 8>{}, std::false_type{});
   if (N == 16) return f(std::integral_constant<int, 16>{}, std::true_type{});
-  if (N < 16) return f(std::integral_constant<int, 16>{}, std::false_type{});
-  if (N == 64) return f(std::integral_constant<int, 64>{}, std::true_type{});
-  return f(std::integral_constant<int, 64>{}, std::false_type{});
+  return f(std::integral_constant<int, 16>{}, std::false_type{});
+}
+template <typename E>
+hipError_t launch_forward_wide(const RouterArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL(router_loss_forward_wide_kernel<E>, dim3(wide_blocks(a.T)), dim3(wide_waves(a.T) * 64), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(router_loss_finish_kernel, dim3(1), dim3(1024), 0, st, a, wide_blocks(a.T));
+  return hipGetLastError();
+}
+template <typename E>
+hipError_t launch_backward_wide(const RouterArgs &a, const int32_t *idx, const float *dw, float gb, float gz, void *dz, hipStream_t st) {
+  hipLaunchKernelGGL(router_loss_backward_wide_kernel<E>, dim3(wide_blocks(a.T)), dim3(wide_waves(a.T) * 64), 0, st, a, idx, dw, gb, gz, dz);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -330,7 +466,7 @@ extern "C" {
 
 size_t mixlora_router_loss_workspace_bytes(const mixlora_router_dims *dims) {
   if (check(dims) != MIXLORA_OK) return 0;
-  return stats_bytes(dims->N) + ((size_t)blocks_of(dims->T) * (3 * dims->N + 2) * 4 + 255) / 256 * 256;
+  return stats_bytes(dims->N) + ((size_t)(dims->N > 16 ? wide_blocks(dims->T) : blocks_of(dims->T)) * (3 * dims->N + 2) * 4 + 255) / 256 * 256;
 }
 
 int mixlora_router_loss_forward(const mixlora_router_dims *dims, const void *logits, const unsigned char *token_mask,
@@ -346,9 +482,12 @@ int mixlora_router_loss_forward(const mixlora_router_dims *dims, const void *log
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   RouterArgs a = args_of(*dims, logits, token_mask, workspace);
   a.idx = topk_idx, a.w = topk_w, a.loss = loss, a.counts = counts;
+  const bool bf16 = dims->dtype == MIXLORA_BF16;
+  if (dims->N > 16)
+    return (bf16 ? launch_forward_wide<bf16_t>(a, st) : launch_forward_wide<float>(a, st)) == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
   const hipError_t e = by_row(dims->N, [&](auto nr, auto full) {
-    return dims->dtype == MIXLORA_BF16 ? launch_forward<bf16_t, nr.value, full.value>(a, st)
-                                       : launch_forward<float, nr.value, full.value>(a, st);
+    return bf16 ? launch_forward<bf16_t, nr.value, full.value>(a, st)
+                : launch_forward<float, nr.value, full.value>(a, st);
   });
   return e == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
 }
@@ -364,8 +503,12 @@ int mixlora_router_loss_backward(const mixlora_router_dims *dims, const void *lo
   if (workspace_bytes < mixlora_router_loss_workspace_bytes(dims)) return MIXLORA_E_WORKSPACE;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const RouterArgs a = args_of(*dims, logits, token_mask, workspace);
+  const bool bf16 = dims->dtype == MIXLORA_BF16;
+  if (dims->N > 16)
+    return (bf16 ? launch_backward_wide<bf16_t>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st)
+                 : launch_backward_wide<float>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st)) == hipSuccess ? MIXLORA_OK : MIXLORA_E_HIP;
   const hipError_t e = by_row(dims->N, [&](auto nr, auto full) {
-    return dims->dtype == MIXLORA_BF16
+    return bf16
                ? launch_backward<bf16_t, nr.value, full.value>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st)
                : launch_backward<float, nr.value, full.value>(a, topk_idx, d_topk_w, d_balance, d_z, dlogits, st);
   });
