@@ -1,0 +1,111 @@
+"""Calls at the edges of what the 4-bit, dropout and router entry points allow: repeated backward passes, scales of the
+adapter that are zero or negative, very many tokens, operands behind 4 GiB."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as orc
+from paper_2404_15159_amd import binding as B
+from test_gpu_q4 import DEV, Q4Linear, check_all, dev, packed, problem
+from test_gpu_router_loss import bound_dlogits, compare, run
+
+pytestmark = pytest.mark.gpu
+SEED, OFFSET = 0x5A5A5A5A12345678, 77
+
+
+@pytest.mark.parametrize("T,p,dtype,q4", [(20, 0.3, "bf16", True), (150, 0.3, "bf16", True), (150, 0.0, "bf16", False),
+                                          (1100, 0.2, "bf16", True), (40, 0.3, "f32", True)])
+def test_backward_again(T, p, dtype, q4):
+    """A backward pass leaves what the forward kept: a second one gives the same bits."""
+    h, W = problem(T, 264, 136, 12, 64, dtype, T)
+    drop = B.make_dropout(p, SEED, OFFSET) if p else None
+    m = Q4Linear(h, packed(W, 64)[0] if q4 else None, 64, dtype, 2.0, drop, W=None if q4 else dev(W, dtype))
+    m.forward()
+    m.backward()
+    first = {k: v.copy() for k, v in m.results().items()}
+    m.dx.t.zero_(), m.dA.t.zero_(), m.dB.t.zero_()
+    m.backward()
+    again = m.results()
+    assert all(np.array_equal(first[n], again[n]) for n in first)
+
+
+@pytest.mark.parametrize("s", [0.0, -1.5, 3e-5])
+@pytest.mark.parametrize("T", [7, 70, 200])
+def test_adapter_scales(T, s):
+    h, W = problem(T, 136, 72, 8, 32, "bf16", T)
+    q4, Wq = packed(W, 32)
+    f = orc.dropout_factors(T, 136, 0.25, SEED, OFFSET)
+    m = Q4Linear(h, q4, 32, "bf16", s, B.make_dropout(0.25, SEED, OFFSET))
+    m.forward()
+    m.backward()
+    check_all(m.results(), h, Wq, float(np.float32(s)), f, "bf16")
+
+
+@pytest.mark.parametrize("q4", [True, False])
+def test_many_tokens(q4):
+    T = 70001
+    h, W = problem(T, 24, 16, 8, 32, "bf16", 3)
+    packed_q4, Wq = packed(W, 32)
+    f = orc.dropout_factors(T, 24, 0.1, SEED, OFFSET)
+    m = Q4Linear(h, packed_q4 if q4 else None, 32, "bf16", 2.0, B.make_dropout(0.1, SEED, OFFSET), W=None if q4 else dev(W, "bf16"))
+    m.forward()
+    m.backward()
+    check_all(m.results(), h, Wq if q4 else W.astype(np.float64), 2.0, f, "bf16")
+
+
+@pytest.mark.parametrize("N,k,dtype", [(5, 2, "f32"), (40, 3, "bf16")])
+def test_router_many_tokens(N, k, dtype):
+    rng = np.random.default_rng(N)
+    T = 30011
+    z = torch.from_numpy(rng.normal(0, 1.5, (T, N)).astype(np.float32)).to(torch.bfloat16).float().numpy()
+    mask, dw = rng.random(T) < 0.6, rng.normal(size=(T, k)).astype(np.float32)
+    got = run(z, mask, k, "topk", dtype, dw)
+    want = orc.router(z, mask, k, "topk", 0.01, 0.001, dw)
+    compare(got, want, N, dtype)
+    assert np.all(np.abs(got["dlogits"] - want["dlogits"]) <= bound_dlogits(z, mask, k, "topk", dw, 1.0, 1.0, 0.01, 0.001, want, dtype))
+
+
+def test_operand_behind_4_gib():
+    """dy and y of 4.3 GB: the products leave the large tiles, and the masked term is added behind an fp32 product.
+    Rows from both ends and both sides of 4 GiB, and the sums over all rows, against 64-bit torch."""
+    T, d_in, d_out, r, p, s = (1 << 20) + 5, 16, 2048, 8, 0.5, 2.0
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    nrm = lambda shape, std: (torch.randn(shape, generator=gen, device=DEV) * std).to(torch.bfloat16)  # noqa: E731
+    x, W, A, Bm = nrm((T, d_in), 1.0), nrm((d_out, d_in), 0.25), nrm((r, d_in), 0.25), nrm((d_out, r), 0.1)
+    dy = torch.empty((T, d_out), dtype=torch.bfloat16, device=DEV)
+    for i in range(0, T, 1 << 17):
+        dy[i:i + (1 << 17)] = nrm((min(1 << 17, T - i), d_out), 1.0)
+    f = torch.from_numpy(orc.dropout_factors(T, d_in, p, SEED, OFFSET)).to(DEV)
+    dims, drop = B.LinearDims(T, d_in, d_out, r, s, B.BF16), B.make_dropout(p, SEED, OFFSET)
+    n = B.mixlora_lora_dropout_workspace_bytes(dims, True)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    y, dx = torch.empty((T, d_out), dtype=torch.bfloat16, device=DEV), torch.empty((T, d_in), dtype=torch.bfloat16, device=DEV)
+    dA, dB = torch.empty((r, d_in), device=DEV), torch.empty((d_out, r), device=DEV)
+    print("case operand behind 4 GiB", flush=True)
+    B.mixlora_lora_dropout_forward(dims, W, A, Bm, drop, x, y, ws, n)
+    torch.cuda.synchronize()
+    B.mixlora_lora_dropout_backward(dims, W, None, A, Bm, drop, x, dy, ws, n, dx, dA, dB)
+    torch.cuda.synchronize()
+    W, A, Bm = W.double(), A.double(), Bm.double()
+    edge = (1 << 32) // (2 * d_out)
+    rows = torch.tensor([0, 1, 777, edge - 1, edge, edge + 1, T - 2, T - 1], device=DEV)
+    xr, fr, dr = x[rows].double(), f[rows], dy[rows].double()
+    want = xr @ W.T + s * (xr * fr) @ A.T @ Bm.T
+    size = xr.abs() @ W.abs().T + s * (xr * fr).abs() @ A.abs().T @ Bm.abs().T
+    assert bool(((y[rows].double() - want).abs() <= 2.0 ** -8 * want.abs() + 64 * 2.0 ** -23 * size).all())
+    want = dr @ W + s * fr * (dr @ Bm @ A)
+    size = dr.abs() @ W.abs() + s * fr * (dr.abs() @ Bm.abs() @ A.abs())
+    assert bool(((dx[rows].double() - want).abs() <= 2.0 ** -8 * want.abs() + 4200 * 2.0 ** -23 * size).all())
+    wA, wB, sA, sB = torch.zeros_like(A), torch.zeros_like(Bm), torch.zeros_like(A), torch.zeros_like(Bm)
+    for i in range(0, T, 1 << 16):
+        j = slice(i, i + (1 << 16))
+        d, xd = dy[j].double(), x[j].double() * f[j]
+        V, P = d @ Bm, xd @ A.T
+        wA += s * V.T @ xd
+        wB += s * d.T @ P
+        sA += s * V.abs().T @ xd.abs()
+        sB += s * d.abs().T @ P.abs()
+    # V and P are sums of 2048 and 16 products; a slice of the rows is summed by MFMA in steps of 16 rows, at most 2^20 / 32 / 16
+    # of them by four waves
+    for got, want, size in ((dA, wA, sA), (dB, wB, sB)):
+        assert bool(((got.double() - want).abs() <= (2064 + 4096) * 2.0 ** -23 * size).all())
