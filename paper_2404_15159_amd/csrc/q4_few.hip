@@ -270,8 +270,8 @@ __device__ __forceinline__ void q4_tile4(const bf16x8_t (&fx)[MT][4], const uint
 }
 
 // In groups of 32 and with four row blocks the scales of four columns, a product per group and block, cost more than scaling
-// the operand: scale x level goes into bf16, exactly for scales of six significant bits (517 tokens 4096 -> 1024 28.8 ->
-// 25.8 us).  A lane takes the four scales of one row.
+// the operand: scale x level goes into bf16, exactly for scales of six significant bits (517 tokens 4096 -> 1024 34.7 ->
+// 23.7 us a pass).  A lane takes the four scales of one row.
 template <int MT>
 __device__ __forceinline__ void q4_tile_scaled(const bf16x8_t (&fx)[MT][4], const uint4 &c, const uint2 &sc, f32x4_t (&acc)[MT]) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));

@@ -5,7 +5,8 @@
 //   dz_ti = g_b a N / n p_ti (F_i - sum_j F_j p_tj) + g_z b 2 / n lse_t p_ti + [i kept] w_ti (dw_ti - sum_j w_tj dw_tj).
 // A token that the mask drops is left out of every sum, whatever its logits are, and gets index -1, weight 0
 // and a zero gradient.  Both directions read the logits once and are bound by a launch's latency (1 MB of
-// logits at 16384 x 16), so a thread takes a token and keeps its row in registers.  Sums over tokens are made on the
+// logits at 16384 x 16), so up to 16 experts a thread takes a token and keeps its row in registers (beyond,
+// a lane takes an expert).  Sums over tokens are made on the
 // vector ALU, counts from ballots.  No sum depends on the order in which workgroups end: their partial sums are added
 // in a fixed order, by a launch of its own.
 #include "common.h"
