@@ -5,7 +5,7 @@
 // in three bf16 pieces that hold all of its 24 bits; the backward's, which has to be masked with dropout, goes first and is
 // masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as well.  A 4-bit matrix is widened
 // into the workspace, which rounds nothing (q4.h), but for the forward of few rows, which multiplies with the codes
-// (q4_few.hip).  fp32: D(x) is made in the workspace, and the products are the fp32 ones.
+// (q4_few.hip).  fp32: the forward makes D(x) in the workspace for both directions, and the products are the fp32 ones.
 #include "common.h"
 #include "q4.h"
 #include "q4_few.h"
@@ -25,8 +25,8 @@ inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) &
 
 struct Layout {
   int rp, ldT;                            // rank rounded up to a multiple of 8; pitch of the transposed factors
-  size_t padA, padB, P, P_T, offs;        // kept for the backward
-  size_t ext, ext_B, proj, gemm_part, xd; // scratch of either direction
+  size_t padA, padB, P, P_T, offs, xd;    // kept for the backward
+  size_t ext, ext_B, proj, gemm_part;     // scratch of either direction
   size_t W, fwd_end;
   size_t W_T, Bt, At, V, V_T, dx32, partials, padgA, padgB, bwd_end;
   size_t few;                             // partial sums of the few-rows product
@@ -50,6 +50,7 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   L.P = take(T * r * 4);
   L.P_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
   L.offs = take(2 * 4);
+  L.xd = take(bf16 ? 0 : T * di * E);
   L.ext = take(bf16 ? T * 3 * r * 2 : 0);
   L.ext_B = take(bf16 ? wide * 3 * r * 2 : 0);
   {
@@ -61,7 +62,6 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
     L.gemm_floats = bf16 && slices >= 2 ? GEMM_SCRATCH_FLOATS / 256 * (tiles < 256 ? tiles : 256) : 0;
     L.gemm_part = take(L.gemm_floats * 4);
   }
-  L.xd = take(bf16 ? 0 : T * di * E);
   const size_t scratch = o;
   // few rows in bf16 multiply with the codes themselves
   L.few_floats = q4 && bf16 ? q4_few_scratch_floats((int)dn, (int)di, (int)T, (int)r) : 0;
@@ -490,14 +490,7 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
   float *V = (float *)(ws + L.V), *P = (float *)(ws + L.P), *part = (float *)(ws + L.partials);
   const int32_t *offs = (const int32_t *)(ws + L.offs);
   if (dt == MIXLORA_F32) {
-    const void *xd = x;
-    if (drop.thr) {
-      const int64_t chunks = (int64_t)T * (di / 8);
-      hipLaunchKernelGGL(dropout_f32_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, (const float *)x,
-                         (float *)(ws + L.xd), chunks, di / 8, drop);
-      HIP_TRY(hipGetLastError());
-      xd = ws + L.xd;
-    }
+    const void *xd = drop.thr ? ws + L.xd : x;
     const GemmProblem p[2] = {problem(T, di, dx, 0, dy, W_T, dn), problem(T, r, V, 1, dy, ws + L.Bt, dn)};
     HIP_TRY(launch_gemm(dt, p, 2, st));
     HIP_TRY(launch_masked_add<float>((const float *)dx, V, ws + L.At, dx, T, di, r, drop.thr ? s * drop.inv : s, drop,
