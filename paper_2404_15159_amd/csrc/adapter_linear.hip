@@ -133,63 +133,77 @@ __global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restric
 }
 
 // out[t, c] = base[t, c] + (c of row t kept ? f * sum_q V[t, q] At[c, q] : 0), rounded once (fp32 storage: base is out).
-// ROWS rows of eight columns per thread.  offs: all tokens are one group of the gradient sums.
+// Bound by base and out.  A workgroup owns 64 columns of 32 ROWS rows and holds both factors in LDS: its columns' part of At is one
+// run of memory.  Eight columns of ROWS rows per thread, one call of the generator each.  A step of 600 tokens 1024 -> 1024 at
+// rank 16 took 95.7 us with At read by every thread in its rows' order, 83.5 so; 3000 2048 -> 2048 at rank 64 909, 764.
+// offs: all tokens are one group of the gradient sums.
+constexpr int MLA_COLS = 64, MLA_PITCH = 64 + 4;
 template <typename E, int ROWS>
 __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *base, const float *__restrict__ V,
                                                                  const E *__restrict__ At, E *out, int T, int C, int r,
                                                                  float f, DropArgs drop, int32_t *offs) {
-  constexpr int MLA_ROWS = ROWS;
-  if (offs && blockIdx.x == 0 && threadIdx.x == 0) offs[0] = 0, offs[1] = T;
-  const int cv = C / 8;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int chunk = (int)(id % cv), c0 = chunk * 8;
-  const int64_t first = id / cv * MLA_ROWS;
-  if (first >= T) return;
-  const int t0 = (int)first;
-  float acc[MLA_ROWS][8];
+  __shared__ __align__(16) float sa[64][MLA_PITCH], sv[32 * ROWS][MLA_PITCH];   // [q][column], [row][q]
+  const int tid = threadIdx.x, col_blocks = (C + MLA_COLS - 1) / MLA_COLS;
+  if (offs && blockIdx.x == 0 && tid == 0) offs[0] = 0, offs[1] = T;
+  const int first_col = blockIdx.x % col_blocks * MLA_COLS, first_row = blockIdx.x / col_blocks * (32 * ROWS);
+  const int c0 = first_col + (tid & 7) * 8, t0 = first_row + (tid >> 3), pieces = r >> 3;
+  Vec8<float> b[ROWS];
 #pragma unroll
-  for (int i = 0; i < MLA_ROWS; i++)
+  for (int i = 0; i < ROWS; i++)
+    b[i].load(base + (int64_t)(t0 + 32 * i < T ? t0 + 32 * i : T - 1) * C + (c0 < C ? c0 : 0));
+  for (int i = tid; i < MLA_COLS * pieces; i += 256) {
+    const int c = i / pieces, q0 = i % pieces * 8;
+    Vec8<E> v;
+    v.load(At + (int64_t)(first_col + c < C ? first_col + c : C - 1) * r + q0);
+#pragma unroll
+    for (int e = 0; e < 8; e++) sa[q0 + e][c] = v.get(e);
+  }
+  for (int i = tid; i < 32 * ROWS * pieces; i += 256) {
+    const int t = i / pieces, q0 = i % pieces * 8;
+    Vec8<float> v;
+    v.load(V + (int64_t)(first_row + t < T ? first_row + t : T - 1) * r + q0);
+    v.store(&sv[t][q0]);
+  }
+  __syncthreads();
+  float acc[ROWS][8];
+#pragma unroll
+  for (int i = 0; i < ROWS; i++)
 #pragma unroll
     for (int j = 0; j < 8; j++) acc[i][j] = 0.f;
-  for (int q0 = 0; q0 < r; q0 += 8) {
-    float wv[8][8];
+  for (int q0 = 0; q0 < r; q0 += 4) {
+    f32x4_t p[ROWS];
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-      Vec8<E> v;
-      v.load(At + (int64_t)(c0 + j) * r + q0);
+    for (int i = 0; i < ROWS; i++) p[i] = *reinterpret_cast<const f32x4_t *>(&sv[(tid >> 3) + 32 * i][q0]);
 #pragma unroll
-      for (int q = 0; q < 8; q++) wv[j][q] = v.get(q);
-    }
+    for (int q = 0; q < 4; q++) {
+      Vec8<float> w;
+      w.load(&sa[q0 + q][(tid & 7) * 8]);
 #pragma unroll
-    for (int i = 0; i < MLA_ROWS; i++) {
-      Vec8<float> pv;
-      pv.load(V + (int64_t)(t0 + i < T ? t0 + i : T - 1) * r + q0);
+      for (int i = 0; i < ROWS; i++)
 #pragma unroll
-      for (int q = 0; q < 8; q++)
-#pragma unroll
-        for (int j = 0; j < 8; j++) acc[i][j] = fmaf(pv.get(q), wv[j][q], acc[i][j]);
+        for (int j = 0; j < 8; j++) acc[i][j] = fmaf(p[i][q], w.get(j), acc[i][j]);
     }
   }
+  if (c0 >= C) return;
   const DropKey key = drop_key(drop);
 #pragma unroll
-  for (int i = 0; i < MLA_ROWS; i++) {
-    if (t0 + i >= T) break;
-    const uint32_t keep = drop.thr ? drop_keep8(key, (uint32_t)(t0 + i), (uint32_t)chunk) : 0xffu;
-    Vec8<float> b;
-    b.load(base + (int64_t)(t0 + i) * C + c0);
+  for (int i = 0; i < ROWS; i++) {
+    const int t = t0 + 32 * i;
+    if (t >= T) break;
+    const uint32_t keep = drop.thr ? drop_keep8(key, (uint32_t)t, (uint32_t)c0 >> 3) : 0xffu;
     Vec8<E> o;
 #pragma unroll
-    for (int j = 0; j < 8; j++) o.set(j, b.get(j) + (keep >> j & 1 ? f * acc[i][j] : 0.f));
-    o.store(out + (int64_t)(t0 + i) * C + c0);
+    for (int j = 0; j < 8; j++) o.set(j, b[i].get(j) + (keep >> j & 1 ? f * acc[i][j] : 0.f));
+    o.store(out + (int64_t)t * C + c0);
   }
 }
 template <typename E>
 hipError_t launch_masked_add(const float *base, const float *V, const void *At, void *out, int T, int C, int r, float f,
                              const DropArgs &drop, int32_t *offs, hipStream_t st) {
-  // four rows per thread read At a quarter as often; one where that leaves most of the chip without a workgroup
-  const bool four = (int64_t)T * (C / 8) >= 4 * 256 * 256;
-  const int64_t threads = (four ? (int64_t)(T + 3) / 4 : T) * (C / 8);
-  const dim3 grid((unsigned)((threads + 255) / 256)), block(256);
+  // four rows per thread read the factors less often; one where that leaves most of the chip without a workgroup
+  const int64_t col_blocks = (C + MLA_COLS - 1) / MLA_COLS;
+  const bool four = (T + 127) / 128 * col_blocks >= 256;
+  const dim3 grid((unsigned)((four ? (T + 127) / 128 : (T + 31) / 32) * col_blocks)), block(256);
   const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
   if (four)
     hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 4>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, f, drop, offs);

@@ -460,7 +460,7 @@ constexpr size_t pp_lds_bytes(int BM) { return (size_t)2 * (BM + PP_BN) * PP_BK 
 // A first segment whose product is masked (launch_gemm_masked): when the K tiles of that segment are done, the
 // accumulators hold it alone, the generator's mask is applied to them, and the other segments follow.  A slice that
 // ends inside it masks what it has.  4096 x 4096 x 4096, rank 16: 105.6 us against 104.9 for the product alone; a
-// kernel that adds the masked term behind the product takes 36 more.
+// product in fp32 and a kernel that adds the masked term behind it take 22 more (rank 64: 37).
 struct NoMask {};
 struct ColumnMask {
   DropArgs drop;
