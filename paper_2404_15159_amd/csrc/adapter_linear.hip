@@ -235,14 +235,6 @@ struct Project {
   DropArgs drop;
 };
 
-// v as the sum of three bf16 values, cut off by truncation; infinities and NaN stay in the first
-__device__ __forceinline__ void three_pieces(float v, float (&pc)[3]) {
-  const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
-  pc[0] = finite ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
-  const float rest = finite ? v - pc[0] : 0.f;
-  pc[1] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-  pc[2] = rest - pc[1];
-}
 __device__ __forceinline__ void store_projection(const Project &a, int t, int q, float v) {
   if (a.drop.thr) v *= a.drop.inv;
   a.P[(int64_t)t * a.r + q] = v;
@@ -363,7 +355,8 @@ size_t project_floats(int T, int K, int r) {
   const int S = project_slices(T, K);
   return S > 1 ? (size_t)S * T * r : 0;
 }
-hipError_t launch_project(Project a, float s, const DropArgs &drop, hipStream_t st) {
+// sliced: the slices, where there are several, are left in a.part for another kernel to add, and their number goes there
+hipError_t launch_project(Project a, float s, const DropArgs &drop, hipStream_t st, int *sliced = nullptr) {
   int e = 0;   // s = m 2^e
   if (std::isfinite(s)) std::frexp(s, &e);
   e = e < -100 ? -100 : e > 100 ? 100 : e;
@@ -397,7 +390,8 @@ hipError_t launch_project(Project a, float s, const DropArgs &drop, hipStream_t 
 #undef MIXLORA_PROJECT_W
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  if (a.S > 1)
+  if (sliced) *sliced = a.S;
+  else if (a.S > 1)
     hipLaunchKernelGGL(project_finish_kernel, dim3((unsigned)(((int64_t)a.T * a.r + 255) / 256)), dim3(256), 0, st, a);
   if (slot >= 0) prof_mark_end(slot, st, 0.0);
   return hipGetLastError();
@@ -444,9 +438,11 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
     return MIXLORA_OK;
   }
   if (L.mid_floats) {
-    HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), D.lora_scale, drop, st));
+    Q4Projection proj{P, 1, 1.f, nullptr, 0};
+    HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), D.lora_scale, drop, st, &proj.S));
+    if (proj.S > 1) proj = Q4Projection{(const float *)(ws + L.proj), proj.S, drop.thr ? drop.inv : 1.f, (bf16_t *)(ws + L.P_T), L.ldT};
     const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.lora_scale, (bf16_t *)y};
-    HIP_TRY(launch_q4_mid(F.q4_matrix(D), a, P, (float *)(ws + L.few), L.mid_floats, st));
+    HIP_TRY(launch_q4_mid(F.q4_matrix(D), a, proj, (float *)(ws + L.few), L.mid_floats, st));
     return MIXLORA_OK;
   }
   if (F.q4) {

@@ -14,9 +14,17 @@ struct Q4Few {
 size_t q4_few_scratch_floats(int n, int K, int T, int r);
 hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop, float *scratch, size_t floats, hipStream_t st);
 
-// The same for more rows, whose projection P [T, r] is there
+// The same for more rows, whose projection is there: S slices [S][T][r], whose sum times f it is.  With PT its three bf16
+// pieces are written there, [3][r][ldT].
+struct Q4Projection {
+  const float *P;
+  int S;
+  float f;
+  bf16_t *PT;
+  int ldT;
+};
 bool q4_mid_ok(int n, int K, int T);
 size_t q4_mid_scratch_floats(int n, int K, int T);
-hipError_t launch_q4_mid(const Q4Matrix &w, const Q4Few &a, const float *P, float *scratch, size_t floats, hipStream_t st);
+hipError_t launch_q4_mid(const Q4Matrix &w, const Q4Few &a, const Q4Projection &P, float *scratch, size_t floats, hipStream_t st);
 
 }  // namespace mixlora

@@ -433,7 +433,7 @@ __global__ __launch_bounds__(512) void q4_slices_kernel(Q4Matrix w, Q4Few a, Q4S
 
 // y = sum of the slices + s (sum of the projection's slices) B^T, in the slices' order.  16 rows x 64 columns per
 // workgroup, four columns of a row per thread.
-__global__ __launch_bounds__(256) void q4_finish_kernel(int n, Q4Few a, Q4Slices z) {
+__global__ __launch_bounds__(256) void q4_finish_kernel(int n, Q4Few a, Q4Slices z, Q4Projection proj) {
   __shared__ float sp[16][64 + 4];
   const int tid = threadIdx.x, T = a.T, r = a.r, t0 = blockIdx.y * 16;
   const int t = t0 + (tid >> 4), c = blockIdx.x * 64 + (tid & 15) * 4;
@@ -455,8 +455,15 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(int n, Q4Few a, Q4Slices
     const int tl = i / r, q = i % r;
     float p = 0.f;
     if (t0 + tl < T)
-      for (int s = 0; s < z.PS; s++) p += z.ppart[((int64_t)s * T + t0 + tl) * r + q];
+      for (int s = 0; s < proj.S; s++) p += proj.P[((int64_t)s * T + t0 + tl) * r + q];
+    p *= proj.f;
     sp[tl][q] = p;
+    if (proj.PT && blockIdx.x == 0 && t0 + tl < T) {
+      float pc[3];
+      three_pieces(p, pc);
+#pragma unroll
+      for (int u = 0; u < 3; u++) proj.PT[((int64_t)u * r + q) * proj.ldT + t0 + tl] = (bf16_t)pc[u];
+    }
   }
   __syncthreads();
   if (!in) return;
@@ -527,20 +534,18 @@ size_t q4_mid_scratch_floats(int n, int K, int T) { return (size_t)plan_slices(n
 #define MIXLORA_S4(PER_) MIXLORA_SLICES(4, 1, PER_)
 #define MIXLORA_S8(PER_) MIXLORA_SLICES(4, 2, PER_)
 
-hipError_t launch_q4_mid(const Q4Matrix &w, const Q4Few &a, const float *P, float *scratch, size_t floats, hipStream_t st) {
+hipError_t launch_q4_mid(const Q4Matrix &w, const Q4Few &a, const Q4Projection &P, float *scratch, size_t floats, hipStream_t st) {
   Q4Slices z = plan_slices(w.n, w.K, a.T);
-  if (!q4_mid_ok(w.n, w.K, a.T) || a.r % 8 || a.r > 64 || w.n % 8 || w.K % 8 || (size_t)z.S * a.T * w.n > floats)
+  if (!q4_mid_ok(w.n, w.K, a.T) || a.r % 8 || a.r > 64 || w.n % 8 || w.K % 8 || P.S < 1 || (size_t)z.S * a.T * w.n > floats)
     return hipErrorInvalidValue;
   const int slot = prof_on() ? prof_mark_begin(PROF_GEMM, st) : -1;
   z.part = scratch;
-  z.ppart = const_cast<float *>(P);   // one slice, read only
-  z.PS = 1;
   const DropArgs drop{};
   const dim3 grid(z.main), block(512);
   MIXLORA_BY_GROUP(MIXLORA_S8);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(q4_finish_kernel, dim3((w.n + 63) / 64, (a.T + 15) / 16), dim3(256), 0, st, w.n, a, z);
+  hipLaunchKernelGGL(q4_finish_kernel, dim3((w.n + 63) / 64, (a.T + 15) / 16), dim3(256), 0, st, w.n, a, z, P);
   if (slot >= 0) prof_mark_end(slot, st, 2.0 * a.T * w.n * w.K);
   return hipGetLastError();
 }
@@ -569,7 +574,8 @@ hipError_t launch_q4_few(const Q4Matrix &w, const Q4Few &a, const DropArgs &drop
     else MIXLORA_BY_GROUP(MIXLORA_S8);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(q4_finish_kernel, dim3((w.n + 63) / 64, (a.T + 15) / 16), dim3(256), 0, st, w.n, a, z);
+    hipLaunchKernelGGL(q4_finish_kernel, dim3((w.n + 63) / 64, (a.T + 15) / 16), dim3(256), 0, st, w.n, a, z,
+                       Q4Projection{z.ppart, z.PS, 1.f, nullptr, 0});
   }
   if (slot >= 0) prof_mark_end(slot, st, 2.0 * a.T * w.n * w.K);
   return hipGetLastError();

@@ -67,4 +67,13 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// v as the sum of three bf16 values, cut off by truncation; infinities and NaN stay in the first
+__device__ __forceinline__ void three_pieces(float v, float (&pc)[3]) {
+  const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
+  pc[0] = finite ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
+  const float rest = finite ? v - pc[0] : 0.f;
+  pc[1] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+  pc[2] = rest - pc[1];
+}
+
 }  // namespace mixlora

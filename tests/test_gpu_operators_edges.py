@@ -109,3 +109,16 @@ def test_operand_behind_4_gib():
     # of them by four waves
     for got, want, size in ((dA, wA, sA), (dB, wB, sB)):
         assert bool(((got.double() - want).abs() <= (2064 + 4096) * 2.0 ** -23 * size).all())
+
+
+@pytest.mark.parametrize("T,d_in,d_out,r,group,p,s", [(150, 1296, 72, 12, 32, 0.3, 2.0), (517, 2056, 40, 64, 128, 0.0, -1.5),
+                                                     (1024, 1160, 136, 8, 64, 0.1, 0.5)])
+def test_sliced_projection(T, d_in, d_out, r, group, p, s):
+    """Tokens and inputs for which the projection comes in slices that the last launch of the forward adds."""
+    h, W = problem(T, d_in, d_out, r, group, "bf16", T)
+    q4, Wq = packed(W, group)
+    f = orc.dropout_factors(T, d_in, p, SEED, OFFSET) if p else np.ones((T, d_in))
+    m = Q4Linear(h, q4, group, "bf16", s, B.make_dropout(p, SEED, OFFSET))
+    m.forward()
+    m.backward()
+    check_all(m.results(), h, Wq, s, f, "bf16")
