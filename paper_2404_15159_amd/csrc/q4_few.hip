@@ -505,13 +505,13 @@ static Q4Slices plan_slices(int n, int K, int T) {
   return z;
 }
 
-// More than 128 rows: while the workgroups are not much more than the chip holds at once; beyond, widening the matrix
-// for the large product costs less than reading x per 64 columns (us, here / widened: 129 tokens 4096 -> 4096 29.7 /
-// 39.5, 512 45.6 / 55.2, 700 71.9 / 63.6; 200 4096 -> 11008 65.3 / 84.6, 300 90.4 / 88.6; 517 4096 -> 1024 27.6 /
-// 33.1, 2000 50.5 / 47.1).
+// More than 128 rows: while the workgroups are not much more than the chip holds at once (not more, over a long contraction);
+// beyond, widening the matrix for the large product costs less than reading x per 64 columns (us, here / widened: 129 tokens
+// 4096 -> 4096 25.3 / 39.6, 512 42.3 / 56.2, 700 64.6 / 63.7; 200 4096 -> 11008 60.2 / 85.5; 517 4096 -> 1024 23.1 /
+// 32.8, 1024 31.6 / 39.3, 2000 47.9 / 47.7; 300 11008 -> 4096 65.2 / 87.0, 600 122 / 108).
 bool q4_mid_ok(int n, int K, int T) {
   const int64_t groups = (q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT;
-  return T > Q4_FEW_ROWS && T <= 1024 && K < 1 << 23 && groups * ((T + 127) / 128) <= 384;
+  return T > Q4_FEW_ROWS && T <= 1024 && K < 1 << 23 && groups * ((T + 127) / 128) <= (K <= 8192 ? 384 : 256);
 }
 size_t q4_mid_scratch_floats(int n, int K, int T) { return (size_t)plan_slices(n, K, T).S * T * n; }
 
