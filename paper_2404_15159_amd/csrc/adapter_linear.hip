@@ -75,7 +75,7 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   L.At = take(di * r * E);
   L.V = take(T * r * 4);
   L.V_T = take(bf16 ? 3 * r * L.ldT * 2 : 0);
-  L.dx32 = take(bf16 && !gemm_masked_ok(D.T, D.d_in, D.d_out) ? T * di * 4 : 0);
+  L.dx32 = take(bf16 && !gemm_masked_ok(D.T, D.d_in, D.d_out, 3 * (int)r) ? T * di * 4 : 0);
   L.partial_floats = bf16 ? adapter_sums_partial_floats((int)r, (int)di, (int)T) + adapter_sums_partial_floats((int)r, (int)dn, (int)T)
                           : group_outer_partial_floats(1, (int)r, (int)di, (int)T) +
                                 group_outer_partial_floats(1, (int)r, (int)dn, (int)T);
@@ -522,12 +522,12 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       p.seg[1] = term;
       p.nseg = 2;
       HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
-    } else if (gemm_masked_ok(T, di, dn)) {
+    } else if (gemm_masked_ok(T, di, dn, 3 * r)) {
       p.seg[0] = term;
       p.seg[1] = frozen;
       p.nseg = 2;
       HIP_TRY(launch_gemm_masked(p, drop, st, gs));
-    } else {   // operands of 4 GiB or more
+    } else {   // operands of 4 GiB or more, the term's included
       p.C = ws + L.dx32;
       p.c_f32 = 1;
       HIP_TRY(launch_gemm(dt, &p, 1, st, gs));

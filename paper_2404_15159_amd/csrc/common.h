@@ -90,9 +90,10 @@ struct GemmScratch {
 // that its sums are taken in the same order.
 hipError_t launch_gemm(int dtype, const GemmProblem *probs, int nprob, hipStream_t st,
                        const GemmScratch &scratch = GemmScratch{nullptr, 0}, int only = -1);
-// bf16: the first segment's product (K <= 192, say) counts only where drop keeps an element of C (row and column of C),
-// unscaled; the others are added to it.  On the large tiles whatever M; operands below 4 GiB (gemm_masked_ok).
-bool gemm_masked_ok(int M, int N, int K);
+// bf16: the first segment's product (K_masked <= 192, say) counts only where drop keeps an element of C (row and column of C),
+// unscaled; the others (K) are added to it.  On the large tiles whatever M; operands of either segment below 4 GiB
+// (gemm_masked_ok).
+bool gemm_masked_ok(int M, int N, int K, int K_masked);
 hipError_t launch_gemm_masked(const GemmProblem &p, const DropArgs &drop, hipStream_t st, const GemmScratch &scratch);
 // the row kernel with the rank-r term of the down projection added, for one or two tokens
 struct FewRank;

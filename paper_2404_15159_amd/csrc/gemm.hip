@@ -1281,8 +1281,9 @@ static hipError_t launch_large(const GemmBatch &b, int nprob, const GemmScratch 
               : launch_pp<256, Mask>(b, nprob, ntail, S, scratch.part, st, mask);
 }
 
-bool gemm_masked_ok(int M, int N, int K) {
-  return (uint64_t)M * K * 2 < (1ull << 32) && (uint64_t)N * K * 2 < (1ull << 32);
+bool gemm_masked_ok(int M, int N, int K, int K_masked) {
+  const uint64_t rows = M > N ? M : N, pitch = K > K_masked ? K : K_masked;
+  return rows * pitch * 2 < (1ull << 32);
 }
 hipError_t launch_gemm_masked(const GemmProblem &p, const DropArgs &drop, hipStream_t st, const GemmScratch &scratch) {
   GemmBatch b;
