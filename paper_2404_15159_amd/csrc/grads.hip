@@ -174,6 +174,9 @@ struct GomBatch {
 // sums in LDS, so that few rows still fill the chip and a slice of the rows leaves a quarter of the partial sums.
 // DROP: of a job with drop.thr != 0, the elements of wide that the generator drops count as zeros (wide row =
 // generator row).
+// An infinite element of wide has to meet the first piece alone: a factor that bf16 holds has zeros for the others, and zero
+// times infinity is NaN.  Taking them out costs six instructions per pair of elements, so a wave makes its sums without, and
+// again with it if one is not a number.
 template <int NQ, int PIECES = 1, bool DROP = false>
 __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(GomBatch batch) {
   constexpr bool BY_ROWS = PIECES == 3;
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 
   DropKey key;
   if constexpr (DROP) key = drop_key(J.drop);
-  auto walk = [&](auto gather) {
+  auto walk = [&](auto gather, auto finite) {   // finite: pieces after the first meet zeros for infinities and NaN
   for (int st = BY_ROWS ? st_lo + wave : st_lo; st < st_hi; st += BY_ROWS ? 4 : 1) {
     const int rbase = base + st * 16 + hi * 8;
     bf16x8_t bq[PIECES][NQ];
@@ -263,15 +266,43 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void group_outer_mfma_kernel(
 #pragma unroll
       for (int p = 0; p < 8; p++) fa[p] = wrow[p][b];
 #pragma unroll
-      for (int pc = 0; pc < PIECES; pc++)
+      for (int pc = 0; pc < PIECES; pc++) {
+        if constexpr (decltype(finite)::value) {
+          if (pc == 1) {
+#pragma unroll
+            for (int p = 0; p < 8; p++) fa[p] = __builtin_isfinite((float)fa[p]) ? fa[p] : (bf16_t)0.f;
+          }
+        }
 #pragma unroll
         for (int j = 0; j < NQ; j++)
           acc[b][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, bq[pc][j], acc[b][j], 0, 0, 0);
+      }
     }
   }
   };
-  if (pair_of_row) walk(std::true_type{});   // (decided outside the loop)
-  else walk(std::false_type{});
+  if constexpr (BY_ROWS) {
+    walk(std::false_type{}, std::false_type{});
+    bool nan = false;
+#pragma unroll
+    for (int b = 0; b < GOM_CB; b++)
+#pragma unroll
+      for (int j = 0; j < NQ; j++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) nan |= __builtin_isunordered(acc[b][j][i], acc[b][j][i + 1]);
+    if (__any(nan)) {
+#pragma unroll
+      for (int b = 0; b < GOM_CB; b++)
+#pragma unroll
+        for (int j = 0; j < NQ; j++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) acc[b][j][i] = 0.f;
+      walk(std::false_type{}, std::true_type{});
+    }
+  } else if (pair_of_row) {   // (decided outside the loop)
+    walk(std::true_type{}, std::false_type{});
+  } else {
+    walk(std::false_type{}, std::false_type{});
+  }
   if constexpr (BY_ROWS) {   // waves 2 and 3 into 0 and 1, then 1 into 0
     extern __shared__ __align__(16) float gom_red[];   // [2][GOM_CB][NQ][4][64][4]
 #pragma unroll
