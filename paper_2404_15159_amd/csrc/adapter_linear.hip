@@ -136,12 +136,13 @@ __global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restric
 // Bound by base and out.  A workgroup owns 64 columns of 32 ROWS rows and holds both factors in LDS: its columns' part of At is one
 // run of memory.  Eight columns of ROWS rows per thread, one call of the generator each.  A step of 600 tokens 1024 -> 1024 at
 // rank 16 took 95.7 us with At read by every thread in its rows' order, 83.5 so; 3000 2048 -> 2048 at rank 64 909, 764.
+// Of V's entries those from `rank` on count as zeros (they fill up a multiple of eight, and are NaN beside an infinite row).
 // offs: all tokens are one group of the gradient sums.
 constexpr int MLA_COLS = 64, MLA_PITCH = 64 + 4;
 template <typename E, int ROWS>
 __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *base, const float *__restrict__ V,
                                                                  const E *__restrict__ At, E *out, int T, int C, int r,
-                                                                 float f, DropArgs drop, int32_t *offs) {
+                                                                 int rank, float f, DropArgs drop, int32_t *offs) {
   __shared__ __align__(16) float sa[64][MLA_PITCH], sv[32 * ROWS][MLA_PITCH];   // [q][column], [row][q]
   const int tid = threadIdx.x, col_blocks = (C + MLA_COLS - 1) / MLA_COLS;
   if (offs && blockIdx.x == 0 && tid == 0) offs[0] = 0, offs[1] = T;
@@ -162,6 +163,10 @@ __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *ba
     const int t = i / pieces, q0 = i % pieces * 8;
     Vec8<float> v;
     v.load(V + (int64_t)(first_row + t < T ? first_row + t : T - 1) * r + q0);
+    if (q0 + 8 > rank) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.set(e, q0 + e < rank ? v.get(e) : 0.f);
+    }
     v.store(&sv[t][q0]);
   }
   __syncthreads();
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(256) void masked_lowrank_add_kernel(const float *ba
   }
 }
 template <typename E>
-hipError_t launch_masked_add(const float *base, const float *V, const void *At, void *out, int T, int C, int r, float f,
+hipError_t launch_masked_add(const float *base, const float *V, const void *At, void *out, int T, int C, int r, int rank, float f,
                              const DropArgs &drop, int32_t *offs, hipStream_t st) {
   // four rows per thread read the factors less often; one where that leaves most of the chip without a workgroup
   const int64_t col_blocks = (C + MLA_COLS - 1) / MLA_COLS;
@@ -206,9 +211,9 @@ hipError_t launch_masked_add(const float *base, const float *V, const void *At, 
   const dim3 grid((unsigned)((four ? (T + 127) / 128 : (T + 31) / 32) * col_blocks)), block(256);
   const int slot = prof_on() ? prof_mark_begin(PROF_OTHER, st) : -1;
   if (four)
-    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 4>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, f, drop, offs);
+    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 4>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, rank, f, drop, offs);
   else
-    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 1>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, f, drop, offs);
+    hipLaunchKernelGGL((masked_lowrank_add_kernel<E, 1>), grid, block, 0, st, base, V, (const E *)At, (E *)out, T, C, r, rank, f, drop, offs);
   if (slot >= 0) prof_mark_end(slot, st, (double)T * C * (4 + sizeof(E)));
   return hipGetLastError();
 }
@@ -228,7 +233,7 @@ GemmProblem problem(int M, int N, void *C, int c_f32, const void *A, const void 
 struct Project {
   const bf16_t *X, *Wq, *Wr;
   int T, K, r, cols, ldT, S;   // S slices of the contraction, of `per` tiles
-  int per;
+  int per, rank;               // entries from rank on fill up a multiple of eight
   float m, b_scale, *P, *part; // part [S][T][r], S > 1
   bf16_t *PT, *ext, *ext_B;
   int32_t *offs;
@@ -237,6 +242,7 @@ struct Project {
 
 __device__ __forceinline__ void store_projection(const Project &a, int t, int q, float v) {
   if (a.drop.thr) v *= a.drop.inv;
+  if (q >= a.rank) v = 0.f;   // a zero row of Wq has made NaN beside an infinite row of X
   a.P[(int64_t)t * a.r + q] = v;
   float pc[3];
   three_pieces(v, pc);
@@ -407,10 +413,10 @@ struct Frozen {
 };
 
 Project project(const Layout &L, char *ws, const void *X, const void *Wq, const void *Wr, int T,
-                int K, int cols, size_t P, size_t PT) {
+                int K, int rank, int cols, size_t P, size_t PT) {
   Project a{};
   a.X = (const bf16_t *)X, a.Wq = (const bf16_t *)Wq, a.Wr = (const bf16_t *)Wr;
-  a.T = T, a.K = K, a.r = L.rp, a.cols = cols, a.ldT = L.ldT;
+  a.T = T, a.K = K, a.r = L.rp, a.rank = rank, a.cols = cols, a.ldT = L.ldT;
   a.P = (float *)(ws + P), a.part = (float *)(ws + L.proj);
   a.PT = (bf16_t *)(ws + PT), a.ext = (bf16_t *)(ws + L.ext), a.ext_B = (bf16_t *)(ws + L.ext_B);
   a.offs = (int32_t *)(ws + L.offs);
@@ -433,15 +439,15 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
   float *P = (float *)(ws + L.P);
   const void *W = F.W;
   if (L.few_floats) {   // (the backward makes the projection itself)
-    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.lora_scale, (bf16_t *)y};
+    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.r, D.lora_scale, (bf16_t *)y};
     HIP_TRY(launch_q4_few(F.q4_matrix(D), a, drop, (float *)(ws + L.few), L.few_floats, st));
     return MIXLORA_OK;
   }
   if (L.mid_floats) {
     Q4Projection proj{P, 1, 1.f, nullptr, 0};
-    HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), D.lora_scale, drop, st, &proj.S));
+    HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, D.r, 0, L.P, L.P_T), D.lora_scale, drop, st, &proj.S));
     if (proj.S > 1) proj = Q4Projection{(const float *)(ws + L.proj), proj.S, drop.thr ? drop.inv : 1.f, (bf16_t *)(ws + L.P_T), L.ldT};
-    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.lora_scale, (bf16_t *)y};
+    const Q4Few a{(const bf16_t *)x, (const bf16_t *)A, (const bf16_t *)B, T, r, D.r, D.lora_scale, (bf16_t *)y};
     HIP_TRY(launch_q4_mid(F.q4_matrix(D), a, proj, (float *)(ws + L.few), L.mid_floats, st));
     return MIXLORA_OK;
   }
@@ -460,10 +466,10 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
     }
     const GemmProblem p[2] = {problem(T, dn, y, 0, x, W, di), problem(T, r, P, 1, xd, A, di)};
     HIP_TRY(launch_gemm(dt, p, 2, st));
-    HIP_TRY(launch_masked_add<float>((const float *)y, P, B, y, T, dn, r, D.lora_scale, DropArgs{}, nullptr, st));
+    HIP_TRY(launch_masked_add<float>((const float *)y, P, B, y, T, dn, r, D.r, D.lora_scale, DropArgs{}, nullptr, st));
     return MIXLORA_OK;
   }
-  HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, dn, L.P, L.P_T), D.lora_scale, drop, st));
+  HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, D.r, dn, L.P, L.P_T), D.lora_scale, drop, st));
   GemmProblem p = problem(T, dn, y, 0, x, W, di);
   p.seg[1] = GemmSeg{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
   p.nseg = 2;
@@ -503,17 +509,17 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
     const void *xd = drop.thr ? ws + L.xd : x;
     const GemmProblem p[2] = {problem(T, di, dx, 0, dy, W_T, dn), problem(T, r, V, 1, dy, ws + L.Bt, dn)};
     HIP_TRY(launch_gemm(dt, p, 2, st));
-    HIP_TRY(launch_masked_add<float>((const float *)dx, V, ws + L.At, dx, T, di, r, drop.thr ? s * drop.inv : s, drop,
+    HIP_TRY(launch_masked_add<float>((const float *)dx, V, ws + L.At, dx, T, di, r, D.r, drop.thr ? s * drop.inv : s, drop,
                                      (int32_t *)(ws + L.offs), st));
     const GoJob go[2] = {GoJob{offs, nullptr, V, (const float *)xd, dA, 1, r, di, 1, T, 1, s},
                          GoJob{offs, nullptr, P, (const float *)dy, dB, 1, r, dn, 1, T, 0, s}};
     HIP_TRY(launch_group_outer(go, 2, part, L.partial_floats, st));
   } else {
     if (L.few_floats) {   // the forward has not kept the projection
-      HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, 0, L.P, L.P_T), s, drop, st));
+      HIP_TRY(launch_project(project(L, ws, x, A, B, T, di, D.r, 0, L.P, L.P_T), s, drop, st));
     }
     // (the term of dx is masked and scaled, the factor V of dA is not)
-    HIP_TRY(launch_project(project(L, ws, dy, ws + L.Bt, ws + L.At, T, dn, di, L.V, L.V_T),
+    HIP_TRY(launch_project(project(L, ws, dy, ws + L.Bt, ws + L.At, T, dn, D.r, di, L.V, L.V_T),
                            drop.thr ? s * drop.inv : s, DropArgs{}, st));
     const GemmScratch gs{L.gemm_floats ? (float *)(ws + L.gemm_part) : nullptr, L.gemm_floats};
     const GemmSeg frozen{dy, W_T, dn, dn, dn}, term{ws + L.ext, ws + L.ext_B, 3 * r, 3 * r, 3 * r};
@@ -531,7 +537,7 @@ int backward(const mixlora_linear_dims &D, const Frozen &F, const void *A, const
       p.C = ws + L.dx32;
       p.c_f32 = 1;
       HIP_TRY(launch_gemm(dt, &p, 1, st, gs));
-      HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, s * drop.inv, drop, nullptr, st));
+      HIP_TRY(launch_masked_add<bf16_t>((const float *)(ws + L.dx32), V, ws + L.At, dx, T, di, r, D.r, s * drop.inv, drop, nullptr, st));
     }
     const GomJob go[2] = {
         GomJob{ws + L.V_T, x, dA, offs, nullptr, 1, r, di, 1, T, L.ldT, 2, 1, drop.thr ? s * drop.inv : s, 0, drop},

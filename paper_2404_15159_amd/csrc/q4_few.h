@@ -7,7 +7,7 @@ namespace mixlora {
 constexpr int Q4_FEW_ROWS = 128;
 struct Q4Few {
   const bf16_t *x, *A, *B;   // [T, K], [r, K], [n, r]; r a multiple of 8
-  int T, r;
+  int T, r, rank;            // entries from rank on fill up r
   float s;
   bf16_t *y;                 // [T, n]
 };

@@ -170,7 +170,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(Q4Matrix w, Q4Few a) {
     float v = red[0][NT][m][ln][u];
 #pragma unroll
     for (int q = 1; q < WAVES; q++) v += red[q][NT][m][ln][u];
-    sp[m * 16 + tok][col] = col < r ? v : 0.f;
+    sp[m * 16 + tok][col] = col < a.rank ? v : 0.f;   // (a zero row of A makes NaN beside an infinite row of x)
   }
   __syncthreads();
 #pragma unroll
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(int n, Q4Few a, Q4Slices
     float p = 0.f;
     if (t0 + tl < T)
       for (int s = 0; s < proj.S; s++) p += proj.P[((int64_t)s * T + t0 + tl) * r + q];
-    p *= proj.f;
+    p = q < a.rank ? p * proj.f : 0.f;
     sp[tl][q] = p;
     if (proj.PT && blockIdx.x == 0 && t0 + tl < T) {
       float pc[3];

@@ -5,7 +5,7 @@ import pytest
 
 from oracle import operators_oracle as orc
 from paper_2404_15159_amd import binding as B
-from test_gpu_q4 import Q4Linear, dev, packed, problem
+from test_gpu_q4 import Q4Linear, dev, packed, problem, rounded
 
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +72,27 @@ def test_sums_of_the_second_factor(T, d_in, d_out, r, p, dtype, q4):
     got, want = run(h, W, p, dtype, q4)
     assert np.isposinf(want["dB"]).any() and np.isneginf(want["dB"]).any()
     same_kind("dB", got["dB"], want["dB"])
+
+
+# ranks that run zero-padded to a multiple of eight, beside ones that do not
+@pytest.mark.parametrize("q4", [True, False])
+@pytest.mark.parametrize("p,dtype", [(0.0, "bf16"), (0.5, "bf16"), (0.0, "f32"), (0.5, "f32")])
+@pytest.mark.parametrize("T,d_in,d_out,r", [(1, 264, 72, 1), (20, 264, 72, 1), (20, 264, 72, 8), (50, 264, 136, 12),
+                                            (100, 264, 136, 20), (150, 1296, 72, 1), (150, 264, 72, 3), (200, 264, 136, 1),
+                                            (300, 264, 136, 35), (1030, 264, 72, 1), (1030, 264, 72, 16)])
+def test_padded_ranks(T, d_in, d_out, r, p, dtype, q4):
+    """An infinite element of x makes x A^T infinite: the rank entries that only fill up a multiple of eight have to stay
+    zeros beside it, or zero times infinity reaches every output of the row.  Likewise dy and dy B."""
+    print(f"case padded rank T={T} {d_in}->{d_out} r={r} p={p} {dtype} q4={q4}", flush=True)
+    h, W = problem(T, d_in, d_out, r, 64, dtype, T + r)
+    h["A"], h["B"] = np.abs(h["A"]) + np.float32(0.0625), np.abs(h["B"]) + np.float32(0.0625)   # one sign over all ranks
+    stay = kept(T, d_in, p)
+    h["x"][T // 2, np.flatnonzero(stay[T // 2])[3]] = np.inf
+    h["x"][T - 1, np.flatnonzero(stay[T - 1])[40]] = -np.inf
+    h["dy"][T // 3, 17], h["dy"][T - 1, 3] = np.inf, -np.inf
+    h = {k: rounded(v, dtype) for k, v in h.items()}
+    got, want = run(h, W, p, dtype, q4)
+    for n in ("y", "dx"):
+        assert np.isposinf(want[n]).any() and np.isneginf(want[n]).any() or T == 1, n
+    for n in got:
+        same_kind(n, got[n], want[n])
