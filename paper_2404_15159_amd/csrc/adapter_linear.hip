@@ -119,10 +119,12 @@ int make_drop(const mixlora_dropout *d, DropArgs &out) {
     if (e_ != hipSuccess) return MIXLORA_E_HIP;         \
   } while (0)
 
-// fp32 storage: out = D(x), eight elements per thread
+// fp32 storage: out = D(x), eight elements per thread.  Workgroups in rows of DROP_GRID_X: a grid dimension holds less than 2^32
+// threads, 2^35 elements.
+constexpr int DROP_GRID_X = 1 << 14;
 __global__ __launch_bounds__(256) void dropout_f32_kernel(const float *__restrict__ x, float *__restrict__ out,
                                                           int64_t chunks, int per_row, DropArgs drop) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = ((int64_t)blockIdx.y * DROP_GRID_X + blockIdx.x) * 256 + threadIdx.x;
   if (i >= chunks) return;
   const uint32_t keep = drop_keep8(drop_key(drop), (uint32_t)(i / per_row), (uint32_t)(i % per_row));
   Vec8<float> v;
@@ -458,9 +460,9 @@ int forward(mixlora_linear_dims D, const Frozen &F, const void *A, const void *B
   if (dt == MIXLORA_F32) {
     const void *xd = x;
     if (drop.thr) {
-      const int64_t chunks = (int64_t)T * (di / 8);
-      hipLaunchKernelGGL(dropout_f32_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, (const float *)x,
-                         (float *)(ws + L.xd), chunks, di / 8, drop);
+      const int64_t chunks = (int64_t)T * (di / 8), blocks = (chunks + 255) / 256;
+      const dim3 grid(blocks < DROP_GRID_X ? (unsigned)blocks : DROP_GRID_X, (unsigned)((blocks + DROP_GRID_X - 1) / DROP_GRID_X));
+      hipLaunchKernelGGL(dropout_f32_kernel, grid, dim3(256), 0, st, (const float *)x, (float *)(ws + L.xd), chunks, di / 8, drop);
       HIP_TRY(hipGetLastError());
       xd = ws + L.xd;
     }

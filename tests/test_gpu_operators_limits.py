@@ -5,7 +5,7 @@ import torch
 
 from oracle import operators_oracle as orc
 from paper_2404_15159_amd import binding as B
-from test_gpu_q4 import DEV
+from test_gpu_q4 import DEV, Q4Linear, check_all, dev, problem
 
 pytestmark = pytest.mark.gpu
 SEED, OFFSET = 0x0F1E2D3C4B5A6978, (9 << 33) + 5
@@ -58,3 +58,14 @@ def test_rank_term_behind_4_gib(T, d_in, d_out):
             wA[:, c] += (s * (V.T @ xd[:, c])).double()
         wB += (s * (d.T @ P)).double()
     assert torch.equal(dA.double(), wA) and torch.equal(dB.double(), wB)
+
+
+def test_dropout_of_more_elements_than_a_grid_row():
+    """fp32: D(x) takes more than one row of its launch (16384 workgroups of 2048 elements)."""
+    T, d_in, d_out, r, p = 4100, 8200, 8, 12, 0.3
+    print(f"case D(x) in grid rows T={T} {d_in}->{d_out} r={r}", flush=True)
+    h, W = problem(T, d_in, d_out, r, 64, "f32", 1)
+    m = Q4Linear(h, None, 64, "f32", 2.0, B.make_dropout(p, SEED, OFFSET), W=dev(W, "f32"))
+    m.forward()
+    m.backward()
+    check_all(m.results(), h, W.astype(np.float64), 2.0, orc.dropout_factors(T, d_in, p, SEED, OFFSET), "f32")
