@@ -381,8 +381,9 @@ typedef struct {
 /* ---- LoRA linear on a 4-bit matrix, and with dropout --------------------------------------------
  *   y = x W^T + s (D(x) A^T) B^T ;  dx = dy W + D'(s (dy B) A),  dA = s (dy B)^T D(x),
  *   dB = s dy^T (D(x) A^T), where D' drops and scales the elements that D does.
- * Shapes, limits (and d_in, d_out < 2^27), workspace rules and errors as in mixlora_lora_linear_forward / _backward
- * (group has to be 32, 64 or 128: MIXLORA_E_SHAPE).  The rank-r factors keep their 24 bits in the sums of dA and dB.
+ * Shapes, limits, workspace rules and errors as in mixlora_lora_linear_forward / _backward; also d_in, d_out < 2^27 and, for
+ * the backward and for ranks off the multiples of 8, the rank so rounded up times either of them < 2^31 (MIXLORA_E_SHAPE, and
+ * 0 bytes; group has to be 32, 64 or 128 likewise).  The rank-r factors keep their 24 bits in the sums of dA and dB.
  * The mixlora_lora_dropout calls take an ordinary frozen matrix (W_T optional as there). */
 MIXLORA_API size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_t group,
                                                      int for_backward);

@@ -86,12 +86,16 @@ Layout make_layout(const mixlora_linear_dims &D, bool q4) {
   return L;
 }
 
-int check_dims(const mixlora_linear_dims *D) {
+// back: of a backward call.  A factor of 2^31 elements is not laid out anew (launch_relayout), which the backward does with
+// both, and the forward where they are padded.
+int check_dims(const mixlora_linear_dims *D, bool back) {
   if (!D) return MIXLORA_E_NULL;
   if (D->dtype != MIXLORA_F32 && D->dtype != MIXLORA_BF16) return MIXLORA_E_DTYPE;
   if (D->T < 1 || D->d_in < 8 || D->d_out < 8 || D->r < 1 || D->r > 64) return MIXLORA_E_SHAPE;
   if (D->d_in % 8 || D->d_out % 8 || D->d_in >= 1 << 27 || D->d_out >= 1 << 27) return MIXLORA_E_SHAPE;
   if ((int64_t)D->T >= (1 << 24)) return MIXLORA_E_SHAPE;
+  const int64_t r = (D->r + 7) & ~7, wide = D->d_in > D->d_out ? D->d_in : D->d_out;
+  if ((back || r != D->r) && r * wide >= (1ll << 31)) return MIXLORA_E_SHAPE;
   return MIXLORA_OK;
 }
 
@@ -568,7 +572,7 @@ int check_pointers(std::initializer_list<const void *> ps) {
 extern "C" {
 
 size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_t group, int for_backward) {
-  if (check_dims(dims) != MIXLORA_OK || !mixlora_q4_scale_bytes(dims->d_out, dims->d_in, group)) return 0;
+  if (check_dims(dims, for_backward != 0) != MIXLORA_OK || !mixlora_q4_scale_bytes(dims->d_out, dims->d_in, group)) return 0;
   const Layout L = make_layout(*dims, true);
   return for_backward ? L.bwd_end : L.fwd_end;
 }
@@ -576,7 +580,7 @@ size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_
 int mixlora_q4_linear_forward(const mixlora_linear_dims *dims, const mixlora_q4 *q4, const void *A, const void *B,
                               const mixlora_dropout *dropout, const void *x, void *y, void *workspace,
                               size_t workspace_bytes, void *stream) {
-  int rc = check_dims(dims);
+  int rc = check_dims(dims, false);
   if (rc) return rc;
   DropArgs drop;
   if ((rc = check_q4(*dims, q4)) || (rc = make_drop(dropout, drop)) || (rc = check_pointers({A, B, x, y, workspace})))
@@ -587,7 +591,7 @@ int mixlora_q4_linear_forward(const mixlora_linear_dims *dims, const mixlora_q4 
 int mixlora_q4_linear_backward(const mixlora_linear_dims *dims, const mixlora_q4 *q4, const void *A, const void *B,
                                const mixlora_dropout *dropout, const void *x, const void *dy, void *workspace,
                                size_t workspace_bytes, void *dx, float *dA, float *dB, void *stream) {
-  int rc = check_dims(dims);
+  int rc = check_dims(dims, true);
   if (rc) return rc;
   DropArgs drop;
   if ((rc = check_q4(*dims, q4)) || (rc = make_drop(dropout, drop)) ||
@@ -598,7 +602,7 @@ int mixlora_q4_linear_backward(const mixlora_linear_dims *dims, const mixlora_q4
 }
 
 size_t mixlora_lora_dropout_workspace_bytes(const mixlora_linear_dims *dims, int for_backward) {
-  if (check_dims(dims) != MIXLORA_OK) return 0;
+  if (check_dims(dims, for_backward != 0) != MIXLORA_OK) return 0;
   const Layout L = make_layout(*dims, false);
   return for_backward ? L.bwd_end : L.fwd_end;
 }
@@ -606,7 +610,7 @@ size_t mixlora_lora_dropout_workspace_bytes(const mixlora_linear_dims *dims, int
 int mixlora_lora_dropout_forward(const mixlora_linear_dims *dims, const void *W, const void *A, const void *B,
                                  const mixlora_dropout *dropout, const void *x, void *y, void *workspace,
                                  size_t workspace_bytes, void *stream) {
-  int rc = check_dims(dims);
+  int rc = check_dims(dims, false);
   if (rc) return rc;
   DropArgs drop;
   if ((rc = make_drop(dropout, drop)) || (rc = check_pointers({W, A, B, x, y, workspace}))) return rc;
@@ -616,7 +620,7 @@ int mixlora_lora_dropout_forward(const mixlora_linear_dims *dims, const void *W,
 int mixlora_lora_dropout_backward(const mixlora_linear_dims *dims, const void *W, const void *W_T, const void *A,
                                   const void *B, const mixlora_dropout *dropout, const void *x, const void *dy,
                                   void *workspace, size_t workspace_bytes, void *dx, float *dA, float *dB, void *stream) {
-  int rc = check_dims(dims);
+  int rc = check_dims(dims, true);
   if (rc) return rc;
   DropArgs drop;
   if ((rc = make_drop(dropout, drop)) || (rc = check_pointers({W, A, B, x, dy, workspace, dx, dA, dB}))) return rc;
