@@ -345,7 +345,7 @@ MIXLORA_API int mixlora_lora_linear_backward(const mixlora_linear_dims *dims, co
  * (0 where that is below 2^-100; NaN, and so every value of the group, where it is 2^127 or more or not a
  * number), the code the nearest level, ties to the even code.  With such scales W' is exact in bf16 and every
  * path below computes with the same W'; scales of more significant bits are allowed, the bf16 products then
- * may see scale x level rounded to bf16.
+ * may see scale x level rounded to bf16 (what multiplies with widened codes does, the forward of few tokens mostly not).
  * Limits: d_out % 8 == 0, d_in % 8 == 0, fewer than 2^31 tiles.  dtype: of W.                    */
 typedef struct {
   void *codes;   /* device, mixlora_q4_code_bytes(d_out, d_in) bytes, 16-byte aligned           */
@@ -384,6 +384,9 @@ typedef struct {
  * Shapes, limits, workspace rules and errors as in mixlora_lora_linear_forward / _backward; also d_in, d_out < 2^27 and, for
  * the backward and for ranks off the multiples of 8, the rank so rounded up times either of them < 2^31 (MIXLORA_E_SHAPE, and
  * 0 bytes; group has to be 32, 64 or 128 likewise).  The rank-r factors keep their 24 bits in the sums of dA and dB.
+ * bf16 elements of x on a 4-bit matrix: up to 2^118 in magnitude; the forward of up to 1024 tokens may add x times level over a
+ * group before it multiplies with the scale, and beyond that such a sum may not be finite where x W^T is.  In float32 every
+ * workspace has room for D(x), T * d_in elements, whether or not a call drops any.
  * The mixlora_lora_dropout calls take an ordinary frozen matrix (W_T optional as there). */
 MIXLORA_API size_t mixlora_q4_linear_workspace_bytes(const mixlora_linear_dims *dims, int32_t group,
                                                      int for_backward);
@@ -415,7 +418,9 @@ MIXLORA_API int mixlora_lora_dropout_backward(const mixlora_linear_dims *dims, c
  * out: loss [3] float32 = {balance + z, balance, z}; counts [N] int32 = pairs per expert; topk_idx [T, k]
  *      int32 and topk_w [T, k] float32.  A token that does not count has indices -1 and weights 0, and its
  *      logits, NaN included, reach nothing.  No token: losses and counts are 0.
- * Limits: 1 <= k <= N <= 64, T * k < 2^24; logits are 16-byte aligned, token_mask need not be. */
+ * Limits: 1 <= k <= N <= 64, T * k < 2^24; every pointer is 16-byte aligned, token_mask need not be.
+ * The block's entry points make their own routing: these calls stand beside them, for a router whose pairs the caller's
+ * program runs, or for its losses and logits' gradient beside a block with an aux_coeff of 0. */
 typedef struct {
   int32_t T, N, k;
   float balance_coeff, z_coeff;

@@ -4,8 +4,8 @@
 // same ones.  bf16: the projection on the rank-r side is made first and rides in the frozen product as an extra K segment,
 // in three bf16 pieces that hold all of its 24 bits; the backward's, which has to be masked with dropout, goes first and is
 // masked in the accumulators.  The gradient sums take the rank-r factor in three pieces as well.  A 4-bit matrix is widened
-// into the workspace, which rounds nothing (q4.h), but for the forward of few rows, which multiplies with the codes
-// (q4_few.hip).  fp32: the forward makes D(x) in the workspace for both directions, and the products are the fp32 ones.
+// into the workspace, which rounds nothing with scales of six bits (q4.h), but for the forward of few rows, which multiplies
+// with the codes (q4_few.hip).  fp32: the forward makes D(x) in the workspace for both directions, and the products are the fp32 ones.
 #include "common.h"
 #include "q4.h"
 #include "q4_few.h"

@@ -3,7 +3,7 @@
 // Bound by reading the codes once, and from some tens of rows on by reading x for every 64 columns.  Codes go from memory
 // to registers as a wavefront's MFMA operand (q4.h) and are widened there, two per instruction; levels are exact in bf16,
 // so x times level is summed in fp32 as it is and a group's sum is multiplied by the group's scale in fp32: nothing is
-// rounded before y (but see q4_tile_scaled).
+// rounded before y (but see q4_tile_scaled).  The sum of a group is at most 768 |x|, which fp32 holds for |x| <= 2^118.
 #include "q4.h"
 #include "q4_few.h"
 #include "dropout.h"
@@ -72,7 +72,7 @@ __device__ __forceinline__ void q4_tile(const bf16x8_t (&fx)[MT][4], const uint4
   }
 }
 
-// ---- up to 64 rows, rank up to 16, no dropout: one launch ---------------------------------------------
+// ---- up to 64 rows (32 of more than 8192 inputs), rank up to 16, no dropout: one launch ---------------------------------------------
 // A workgroup owns NT tiles' rows (16 NT columns of y) over the whole contraction, its eight wavefronts every
 // eighth tile of it; MT blocks of 16 rows of x.  Every workgroup makes the projection x A^T itself (128 KB of A at
 // 16 x 4096, out of L2): that costs less than a launch in front of this one.  Nothing is requested ahead within a
@@ -212,8 +212,14 @@ static hipError_t launch_few(const Q4Matrix &w, const Q4Few &a, hipStream_t st) 
 }
 template <int MT, int PER, bool ONE>
 static hipError_t launch_few_n(const Q4Matrix &w, const Q4Few &a, hipStream_t st) {
-  // as many tiles per workgroup as leave the chip one round of workgroups (4096 -> 11008 with one, two, three: 11.3,
-  // 9.4, 7.8 us; 4096 -> 4096 with one and three: 5.4, 6.8)
+  // as many tiles per workgroup as leave the chip one round of workgroups.  One, two, three of them at 1 | 24 | 64 tokens, us,
+  // with the codes in memory, not in a cache:
+  //   4096 -> 4096,   256 tiles   6.6  6.9  7.8 |  9.7 10.4 11.8 | 14.9 15.2 17.1
+  //   5120 -> 5120,   320 tiles  11.7  8.5  9.7 | 18.4 13.2 14.7 | 29.8 19.8 22.2
+  //   4096 -> 8192,   512 tiles  10.0  7.5  8.3 | 15.2 11.0 12.3 | 26.8 17.0 17.7
+  //   4096 -> 11008,  688 tiles  13.3 11.6  8.8 | 20.8 18.6 12.8 | 36.9 28.4 18.6
+  // More than 768 tiles are more than a round of three, which is where two would be ahead until they need a third round:
+  //   4096 -> 14336,  896 tiles  16.8 12.0 14.4 | 26.3 19.6 21.6 | 47.8 29.9 31.5
   const int64_t tiles = q4_row_blocks(w.n);
   if (tiles <= 256) return launch_few<1, MT, PER, ONE>(w, a, st);
   if (tiles <= 512) return launch_few<2, MT, PER, ONE>(w, a, st);
@@ -507,7 +513,7 @@ static Q4Slices plan_slices(int n, int K, int T) {
 
 // More than 128 rows: while the workgroups are not much more than the chip holds at once (not more, over a long contraction);
 // beyond, widening the matrix for the large product costs less than reading x per 64 columns (us, here / widened: 129 tokens
-// 4096 -> 4096 25.3 / 39.6, 512 42.3 / 56.2, 700 64.6 / 63.7; 200 4096 -> 11008 60.2 / 85.5; 517 4096 -> 1024 23.1 /
+// 4096 -> 4096 25.3 / 39.6, 512 42.3 / 56.2, 700 64.6 / 63.7; 200 4096 -> 11008 60.2 / 85.5; 517 4096 -> 1024 21.9 /
 // 32.8, 1024 31.6 / 39.3, 2000 47.9 / 47.7; 300 11008 -> 4096 65.2 / 87.0, 600 122 / 108).
 bool q4_mid_ok(int n, int K, int T) {
   const int64_t groups = (q4_row_blocks(n) + Q4S_NT - 1) / Q4S_NT;
